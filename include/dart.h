@@ -356,6 +356,74 @@ int dart_profile_read(dart_ctx *ctx, float *ms, int32_t *launches, const char **
 int dart_pivots_static(const void *keys, int B, int S, int d, int vis_offset, int n_vis, int n_pivot,
                        int32_t *pivot_idx, int device, void *stream);
 
+/*
+ * What stands around the reduction in a serving engine: the rows of queries and keys that it reads, and the paged cache that
+ * takes what it keeps.  None of these entry points needs a context.  Values are 16 bits wide (dtype), sums and rotations are held in
+ * fp32 and rounded once.  A row holds its heads side by side (heads * head_dim values); rows are `stride` values apart, a
+ * multiple of 8, so that they may be columns of a wider buffer (a projection's output).
+ */
+#define DART_BF16 0
+#define DART_FP16 1
+
+/* A position rotation.  With half = rot_dim / 2 and angle_i = pos * inv_freq[i] (i < half), a head x becomes
+ *   interleaved == 0:  x[i] cos_i - x[i + half] sin_i,  x[i + half] cos_i + x[i] sin_i
+ *   interleaved != 0:  the same with elements 2i and 2i + 1;   elements from rot_dim on stay.
+ * Angles are taken in fp64, so that far and negative positions lose nothing. */
+typedef struct {
+    const float *inv_freq; /* [rot_dim / 2] device */
+    const int64_t *pos;    /* device: [n_axes][pos_stride], row n's position(s) at n, n + pos_stride, ... */
+    int64_t pos_stride;    /* values from axis to axis (>= n_rows; any with one axis) */
+    int32_t rot_dim;       /* a multiple of 16, at most head_dim; 0: no rotation */
+    int32_t interleaved;
+    int32_t n_axes;        /* 0 or 1: one position a row; 2, 3: time, height, width of vision tokens: the first section[0] pairs turn
+                              by the first axis, the next section[1] by the second, ... */
+    int32_t section[3];    /* with n_axes > 1: pairs per axis, rot_dim / 2 in all */
+} dart_rope;
+
+/*
+ * The norm of every head of the queries and keys and their rotation, in one pass: y = x * rsqrt(mean(x^2) + eps) * weight, then the
+ * rotation.  The keys' rows, heads side by side, are what dart_reduce scores.
+ *   q, k           [n_rows] rows of n_q_heads / n_k_heads heads, device, 16-byte aligned; either may have 0 heads (then its
+ *                  pointers are not looked at)
+ *   q_weight, k_weight [head_dim] of the rows' type, device, 16-byte aligned, or NULL: no norm
+ *   rope           NULL or rot_dim 0: no rotation
+ *   q_out, k_out   rows as q and k; may be q and k themselves (same pointer and stride) or columns of one buffer, else they must
+ *                  not share a byte with any input or with each other
+ * Limits: head_dim a multiple of 8 up to 256; at most 65536 heads in all; n_rows 0 does nothing.
+ * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED (dtype), CUDA.
+ */
+int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k, int64_t k_stride, int n_k_heads, int n_rows,
+                   int head_dim, int dtype, const void *q_weight, const void *k_weight, float eps, const dart_rope *rope,
+                   void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream);
+
+/* A paged cache of keys and values: each [n_pages][n_heads][page_size][head_dim], dense, 16-byte aligned, on `device`.  A sequence's
+ * token number s lies in page table[sequence][s / page_size] at place s % page_size. */
+typedef struct {
+    void *k, *v;
+    int32_t n_pages, n_heads, page_size, head_dim;
+    int32_t dtype, device;
+} dart_cache;
+
+/*
+ * Put rows of keys and values into the pages of a cache, the keys normalised and rotated on the way.  Packed row n of sequence b
+ * (cu_rows[b] <= n < cu_rows[b + 1]) goes to slot start[b] + n - cu_rows[b] of the sequence.  With idx = the out_idx of a reduction
+ * these are the rows that it kept of a layer's S rows a sample (packed without padding by its cu_seqlens, positions by its out_pos).
+ *   k, v        rows of cache->n_heads heads, device, 16-byte aligned: n_rows of them, or with idx n_seq * S
+ *   cu_rows     [n_seq + 1] int32 device, ascending, or NULL: n_rows / n_seq rows each.  Rows before cu_rows[0] or from cu_rows[n_seq]
+ *               on are not handled
+ *   idx         NULL: packed row n is row n of k and v; else [n_rows] int32 device: it is row b * S + idx[n]
+ *   table       [n_seq][table_stride] int32 device; only the entries of written slots are read.  No two rows may have the same slot
+ *   start       [n_seq] int32 device: tokens that the cache already holds, or NULL: none
+ *   k_weight, eps, rope  as in dart_norm_rope, for the keys; rope->pos is by packed row; NULL: the slot is the position
+ *   status      [4] int32 device, or NULL.  A row whose slot is outside its table row, whose page is outside the cache or whose idx is
+ *               outside [0, S) is left out, and status[0] becomes DART_ERR_CHECK
+ * cache->page_size may be any positive number here.  n_rows 0 does nothing.
+ * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS (the cache overlaps k or v), UNSUPPORTED, CUDA.
+ */
+int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int n_seq,
+                      int n_rows, const int32_t *cu_rows, const int32_t *idx, int S, const int32_t *table, int table_stride,
+                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, int32_t *status, void *stream);
+
 const char *dart_strerror(int code);
 int dart_version(void);
 

@@ -1,0 +1,168 @@
+// Host side of the entry points around the reduction: rows of queries and keys on their way to it, the cache of what it keeps,
+// and the attention that reads the cache.  Argument checks and launches; nothing here allocates.
+#include "../../include/dart.h"
+
+#include <math.h>
+
+#include "dart_host.cuh"
+#include "dart_rows.cuh"
+
+namespace {
+
+bool misaligned(const void *p, unsigned to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+// Whether two sets of rows share a byte: n rows of `width` bytes, `stride` bytes apart.  Columns of one buffer do not.
+bool rows_overlap(const void *a, long long na, long long sa, long long wa, const void *b, long long nb, long long sb, long long wb)
+{
+    if (!a || !b || na == 0 || nb == 0 || !overlaps(a, (size_t)((na - 1) * sa + wa), b, (size_t)((nb - 1) * sb + wb))) return false;
+    if (sa != sb || sa <= 0) return true;
+    const long long d = ((long long)((uintptr_t)b - (uintptr_t)a) % sa + sa) % sa;
+    return d < wa || sa - d < wb;
+}
+
+int check_rope(const dart_rope *r, int head_dim, int n_rows, bool need_pos)
+{
+    if (!r || r->rot_dim == 0) return DART_OK;
+    if (!r->inv_freq || (need_pos && !r->pos)) return DART_ERR_NULL;
+    if (r->rot_dim < 0 || r->rot_dim % 16 != 0 || r->rot_dim > head_dim || r->n_axes < 0 || r->n_axes > 3) return DART_ERR_BAD_SHAPE;
+    if (r->n_axes > 1) {
+        if (r->pos && r->pos_stride < n_rows) return DART_ERR_BAD_SHAPE;
+        long long sum = 0;
+        for (int a = 0; a < r->n_axes; ++a) {
+            if (r->section[a] < 0) return DART_ERR_BAD_SHAPE;
+            sum += r->section[a];
+        }
+        if (sum != r->rot_dim / 2) return DART_ERR_BAD_SHAPE;
+    }
+    if (misaligned(r->inv_freq, 4) || misaligned(r->pos, 8)) return DART_ERR_ALIGN;
+    return DART_OK;
+}
+
+void set_rope(dart::rows::Params &p, const dart_rope *r)
+{
+    p.half = 0;
+    if (!r || r->rot_dim == 0) return;
+    p.half = r->rot_dim / 2, p.interleaved = r->interleaved != 0;
+    p.n_axes = r->n_axes > 1 ? r->n_axes : 1;
+    p.sec0 = r->n_axes > 1 ? r->section[0] : p.half;
+    p.sec01 = r->n_axes > 2 ? r->section[0] + r->section[1] : p.half; // (two axes: no pair turns by a third)
+    p.inv_freq = r->inv_freq, p.pos = r->pos, p.pos_stride = r->pos_stride;
+}
+
+bool known_type(int dtype) { return dtype == DART_BF16 || dtype == DART_FP16; }
+bool head_rows_ok(int heads, int D, long long stride, int n_rows) { return heads >= 0 && (n_rows <= 1 || stride >= (long long)heads * D) && stride % 8 == 0 && stride >= 0; }
+
+// Blocks of 256 threads.  Few rows: one round of heads per block, a row's heads over several blocks.  Many rows: up to eight rows
+// a block, so that a thread has several rounds to overlap and the rows' angles serve all heads.
+template <typename T, bool kPaged>
+int launch_rows(dart::rows::Params &p, cudaStream_t st)
+{
+    using namespace dart::rows;
+    const int H = p.side[0].heads + p.side[1].heads;
+    const int pairs = (p.D / 8 + 1) / 2, kh = pairs <= 4 ? 4 : pairs <= 8 ? 8 : 16;
+    const int groups = kThreads / kh;
+    const long long rounds = ((long long)p.n_rows * H + groups - 1) / groups; // of a block
+    p.heads_per_block = H, p.rows_per_block = 1;
+    if (rounds <= 148 * 8)
+        p.heads_per_block = H < groups ? H : groups;
+    else
+        while (p.rows_per_block < kMaxRows && p.rows_per_block * H < 8 * groups) p.rows_per_block *= 2;
+    const dim3 grid((unsigned)((p.n_rows + p.rows_per_block - 1) / p.rows_per_block), (unsigned)((H + p.heads_per_block - 1) / p.heads_per_block));
+    if (grid.y > 65535u) return DART_ERR_BAD_SHAPE;
+    cudaError_t e = kh == 4    ? launch_next(head_rows_kernel<T, 4, kPaged>, grid, kThreads, 0, st, p)
+                    : kh == 8  ? launch_next(head_rows_kernel<T, 8, kPaged>, grid, kThreads, 0, st, p)
+                               : launch_next(head_rows_kernel<T, 16, kPaged>, grid, kThreads, 0, st, p);
+    const cudaError_t e2 = cudaGetLastError();
+    return e == cudaSuccess && e2 == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+}
+
+int check_cache(const dart_cache *c)
+{
+    if (!c || !c->k || !c->v) return DART_ERR_NULL;
+    if (c->n_pages < 1 || c->n_heads < 1 || c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0 || c->page_size < 1) return DART_ERR_BAD_SHAPE;
+    if (!known_type(c->dtype)) return DART_ERR_UNSUPPORTED;
+    if (misaligned(c->k, 16) || misaligned(c->v, 16)) return DART_ERR_ALIGN;
+    return DART_OK;
+}
+
+size_t cache_bytes(const dart_cache *c) { return (size_t)c->n_pages * c->n_heads * c->page_size * c->head_dim * 2; }
+
+} // namespace
+
+extern "C" {
+
+int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k, int64_t k_stride, int n_k_heads, int n_rows,
+                   int head_dim, int dtype, const void *q_weight, const void *k_weight, float eps, const dart_rope *rope,
+                   void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream)
+{
+    if (n_rows < 0 || n_q_heads < 0 || n_k_heads < 0 || n_q_heads + (long long)n_k_heads < 1 || n_q_heads + (long long)n_k_heads > 65536 ||
+        head_dim < 8 || head_dim > 256 || head_dim % 8 != 0 || !(eps >= 0.0f) || isinf(eps))
+        return DART_ERR_BAD_SHAPE;
+    if (!known_type(dtype)) return DART_ERR_UNSUPPORTED;
+    if (n_rows == 0) return DART_OK;
+    if ((n_q_heads && (!q || !q_out)) || (n_k_heads && (!k || !k_out))) return DART_ERR_NULL;
+    if (!head_rows_ok(n_q_heads, head_dim, q_stride, n_rows) || !head_rows_ok(n_q_heads, head_dim, qo_stride, n_rows) ||
+        !head_rows_ok(n_k_heads, head_dim, k_stride, n_rows) || !head_rows_ok(n_k_heads, head_dim, ko_stride, n_rows))
+        return DART_ERR_BAD_SHAPE;
+    int rc = check_rope(rope, head_dim, n_rows, true);
+    if (rc != DART_OK) return rc;
+    if (!n_q_heads) q = q_out = nullptr, q_weight = nullptr;
+    if (!n_k_heads) k = k_out = nullptr, k_weight = nullptr;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) || misaligned(q_weight, 16) || misaligned(k_weight, 16))
+        return DART_ERR_ALIGN;
+    const long long wq = 2ll * n_q_heads * head_dim, wk = 2ll * n_k_heads * head_dim;
+    const bool q_in_place = q_out == q && qo_stride == q_stride, k_in_place = k_out == k && ko_stride == k_stride;
+    if ((!q_in_place && rows_overlap(q_out, n_rows, 2 * qo_stride, wq, q, n_rows, 2 * q_stride, wq)) ||
+        (!k_in_place && rows_overlap(k_out, n_rows, 2 * ko_stride, wk, k, n_rows, 2 * k_stride, wk)) ||
+        rows_overlap(q_out, n_rows, 2 * qo_stride, wq, k, n_rows, 2 * k_stride, wk) ||
+        rows_overlap(k_out, n_rows, 2 * ko_stride, wk, q, n_rows, 2 * q_stride, wq) ||
+        rows_overlap(q_out, n_rows, 2 * qo_stride, wq, k_out, n_rows, 2 * ko_stride, wk))
+        return DART_ERR_ALIAS;
+    DeviceGuard g(device);
+    if (!g.ok) return DART_ERR_CUDA;
+    dart::rows::Params p = {};
+    p.side[0] = {(const char *)q, (char *)q_out, (const char *)q_weight, 2 * q_stride, 2 * qo_stride, n_q_heads, true};
+    p.side[1] = {(const char *)k, (char *)k_out, (const char *)k_weight, 2 * k_stride, 2 * ko_stride, n_k_heads, true};
+    p.n_rows = n_rows, p.D = head_dim, p.eps = eps;
+    set_rope(p, rope);
+    return dtype == DART_BF16 ? launch_rows<__nv_bfloat16, false>(p, (cudaStream_t)stream) : launch_rows<__half, false>(p, (cudaStream_t)stream);
+}
+
+int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int n_seq,
+                      int n_rows, const int32_t *cu_rows, const int32_t *idx, int S, const int32_t *table, int table_stride,
+                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, int32_t *status, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != DART_OK) return rc;
+    if (n_rows < 0 || n_seq < 1 || table_stride < 1 || (idx && S < 1) || (!cu_rows && n_rows % n_seq != 0) || !(eps >= 0.0f) || isinf(eps) ||
+        cache->n_heads > 32768)
+        return DART_ERR_BAD_SHAPE;
+    if (n_rows == 0) return DART_OK;
+    if (!k || !v || !table) return DART_ERR_NULL;
+    const long long n_src = idx ? (long long)n_seq * S : n_rows;
+    const int D = cache->head_dim, Hk = cache->n_heads;
+    if (!head_rows_ok(Hk, D, k_stride, n_src > 1 ? 2 : 1) || !head_rows_ok(Hk, D, v_stride, n_src > 1 ? 2 : 1)) return DART_ERR_BAD_SHAPE;
+    rc = check_rope(rope, D, n_rows, false);
+    if (rc != DART_OK) return rc;
+    if (rope && rope->rot_dim && !rope->pos && rope->n_axes > 1) return DART_ERR_NULL; // a slot is a position on one axis only
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_weight, 16) || misaligned(cu_rows, 4) || misaligned(idx, 4) || misaligned(table, 4) ||
+        misaligned(start, 4) || misaligned(status, 4))
+        return DART_ERR_ALIGN;
+    const size_t all = cache_bytes(cache), row = 2 * (size_t)Hk * D;
+    const size_t kb = (size_t)(n_src - 1) * 2 * k_stride + row, vb = (size_t)(n_src - 1) * 2 * v_stride + row;
+    if (overlaps(cache->k, all, cache->v, all) || overlaps(cache->k, all, k, kb) || overlaps(cache->k, all, v, vb) || overlaps(cache->v, all, k, kb) ||
+        overlaps(cache->v, all, v, vb))
+        return DART_ERR_ALIAS;
+    DeviceGuard g(cache->device);
+    if (!g.ok) return DART_ERR_CUDA;
+    dart::rows::Params p = {};
+    p.side[0] = {(const char *)k, (char *)cache->k, (const char *)k_weight, 2 * k_stride, 0, Hk, true};
+    p.side[1] = {(const char *)v, (char *)cache->v, nullptr, 2 * v_stride, 0, Hk, false};
+    p.n_rows = n_rows, p.D = D, p.eps = eps;
+    set_rope(p, rope);
+    p.n_seq = n_seq, p.per_seq = cu_rows ? 0 : n_rows / n_seq, p.S = S, p.table_stride = table_stride, p.page_size = cache->page_size;
+    p.n_pages = cache->n_pages, p.cu = cu_rows, p.idx = idx, p.table = table, p.start = start, p.status = status;
+    return cache->dtype == DART_BF16 ? launch_rows<__nv_bfloat16, true>(p, (cudaStream_t)stream) : launch_rows<__half, true>(p, (cudaStream_t)stream);
+}
+
+} // extern "C"

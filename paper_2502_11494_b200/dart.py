@@ -29,9 +29,10 @@ EXPORTS = (
     "dart_create", "dart_destroy", "dart_set_shape", "dart_reduce", "dart_reduce_ex", "dart_reduce_host",
     "dart_status", "dart_status_detail", "dart_last_cuda_error", "dart_workspace_bytes", "dart_launch_count",
     "dart_profile_enable", "dart_profile_read", "dart_strerror", "dart_version", "dart_pivots_static",
-    "dart_gather_rows",
+    "dart_gather_rows", "dart_norm_rope", "dart_cache_append",
 )
 DART_STATIC_MAX_ROWS = 262144
+DART_BF16, DART_FP16 = 0, 1
 
 
 class dart_desc(ctypes.Structure):
@@ -54,6 +55,18 @@ class dart_debug(ctypes.Structure):
     _fields_ = [("l1", ctypes.c_void_p), ("ssq", ctypes.c_void_p), ("pivot_idx", ctypes.c_void_p),
                 ("sim", ctypes.c_void_p), ("eps", ctypes.c_void_p), ("keep", ctypes.c_void_p),
                 ("owner", ctypes.c_void_p)]
+
+
+class dart_rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3)]
+
+
+class dart_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("device", ctypes.c_int32)]
 
 
 class DartError(RuntimeError):
@@ -93,6 +106,11 @@ def lib() -> ctypes.CDLL:
                                         ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_int)]
         L.dart_pivots_static.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32p, i32, vp]
         L.dart_gather_rows.argtypes = [vp, i32p, i32, i32, i32, i32, vp, i32, vp]
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.dart_norm_rope.argtypes = [vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, f32, ctypes.POINTER(dart_rope), vp, i64,
+                                     vp, i64, i32, vp]
+        L.dart_cache_append.argtypes = [ctypes.POINTER(dart_cache), vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i32, vp, vp, f32,
+                                        ctypes.POINTER(dart_rope), vp, vp]
         L.dart_strerror.argtypes = [i32]
         L.dart_strerror.restype = ctypes.c_char_p
         L.dart_version.argtypes = []
@@ -149,6 +167,20 @@ def dart_pivots_static(keys, B, S, d, vis_offset, n_vis, n_pivot, pivot_idx, dev
 def dart_gather_rows(src, idx, B, S, S_out, row_bytes, out, device, stream) -> int:
     """Context-free row gather by a packed index list (raw device pointers); see include/dart.h."""
     return lib().dart_gather_rows(src, idx, B, S, S_out, row_bytes, out, device, stream)
+
+
+def dart_norm_rope(q, q_stride, n_q_heads, k, k_stride, n_k_heads, n_rows, head_dim, dtype, q_weight, k_weight, eps,
+                   rope: Optional[dart_rope], q_out, qo_stride, k_out, ko_stride, device, stream) -> int:
+    """Norm of each head and position rotation of queries and keys (raw device pointers); see include/dart.h."""
+    return lib().dart_norm_rope(q, q_stride, n_q_heads, k, k_stride, n_k_heads, n_rows, head_dim, dtype, q_weight, k_weight,
+                                eps, rope, q_out, qo_stride, k_out, ko_stride, device, stream)
+
+
+def dart_cache_append(cache: Optional[dart_cache], k, k_stride, v, v_stride, n_seq, n_rows, cu_rows, idx, S, table, table_stride,
+                      start, k_weight, eps, rope: Optional[dart_rope], status, stream) -> int:
+    """Rows of keys and values into the pages of a cache (raw device pointers); see include/dart.h."""
+    return lib().dart_cache_append(cache, k, k_stride, v, v_stride, n_seq, n_rows, cu_rows, idx, S, table, table_stride, start,
+                                   k_weight, eps, rope, status, stream)
 
 
 def dart_status(ctx) -> int:
@@ -266,3 +298,171 @@ class Dart:
 
     def status(self) -> int:
         return dart_status(self._h)
+
+
+# ---- around the reduction: rotated rows, the paged cache -------------------------------------------
+
+class Rope:
+    """A position rotation: the first ``2 * len(inv_freq)`` elements of a head turn by ``pos * inv_freq``, pairs being
+    ``(i, i + half)`` or, ``interleaved``, ``(2i, 2i + 1)``.  ``sections``: pairs per position axis (vision tokens in time,
+    height and width)."""
+
+    def __init__(self, inv_freq, interleaved=False, sections=None):
+        import torch
+
+        if not (inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()):
+            raise ValueError("inv_freq must be a contiguous fp32 CUDA vector")
+        self.inv_freq, self.axes = inv_freq, len(sections) if sections is not None else 1
+        if not 1 <= self.axes <= 3:
+            raise ValueError("one to three sections")
+        self._c = (inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved), self.axes,
+                   tuple(int(n) for n in sections) + (0,) * (3 - self.axes) if sections is not None else (0, 0, 0))
+
+    def at(self, pos, n_rows, device):
+        """The C struct for rows at ``pos`` ([n_rows], or [axes, n_rows]; None where the callee has its own)."""
+        import torch
+
+        inv_freq, rot_dim, interleaved, axes, section = self._c
+        if device != self.inv_freq.device:
+            raise ValueError("inv_freq and the rows must be on the same device")
+        stride = 0
+        if pos is not None:
+            if not (pos.dtype == torch.int64 and pos.device == device and pos.numel() == axes * n_rows
+                    and pos.shape[-1] == n_rows and (n_rows <= 1 or pos.stride(-1) == 1)):
+                raise ValueError("pos must be int64 [%s%d] on the rows' device" % ("%d, " % axes if axes > 1 else "", n_rows))
+            stride = pos.stride(0) if axes > 1 else n_rows
+        return dart_rope(inv_freq, pos.data_ptr() if pos is not None else None, stride, rot_dim, interleaved, axes, section)
+
+
+def _dtype_code(dtype):
+    import torch
+
+    if dtype == torch.bfloat16:
+        return DART_BF16
+    if dtype == torch.float16:
+        return DART_FP16
+    raise ValueError("rows must be bf16 or fp16")
+
+
+def _head_rows(t, name, dtype, device, n_rows=None):
+    """[rows, heads, D] with the heads of a row side by side -> values from row to row."""
+    if t.dim() != 3 or t.dtype != dtype or t.device != device or not t.is_cuda or (n_rows is not None and t.shape[0] != n_rows):
+        raise ValueError("%s must be a CUDA tensor [rows, heads, head_dim] of the same type, device and rows as the others" % name)
+    n, h, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+        raise ValueError("%s: the heads of a row must lie side by side" % name)
+    return t.stride(0) if n > 1 else h * d
+
+
+def _vector(t, name, size, dtype, device):
+    if t is not None and not (t.dtype == dtype and t.device == device and t.shape == (size,) and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous vector of %d values of type %s on %s" % (name, size, dtype, device))
+    return t.data_ptr() if t is not None else None
+
+
+def _stream(stream, device):
+    import torch
+
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, out=None, stream=None):
+    """Norm of each head (``q_weight`` / ``k_weight`` [D], None: no norm) and rotation of queries [N, Hq, D] and keys [N, Hk, D]
+    (either may be None) in one pass.  ``pos``: int64 [N], or [axes, N].  ``out``: (q_out, k_out), which may be q and k
+    themselves.  Returns (q_out, k_out)."""
+    import torch
+
+    one = q if q is not None else k
+    if one is None:
+        raise ValueError("queries or keys are needed")
+    dtype, dev = one.dtype, one.device
+    code, n, D = _dtype_code(dtype), one.shape[0], one.shape[-1]
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=dtype, device=dev) if t is not None else None for t in (q, k))
+    args = []
+    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
+        if t is None:
+            args.append((None, 0, 0, None, 0))
+            continue
+        stride = _head_rows(t, name, dtype, dev, n)
+        if t.shape[2] != D or o is None or o.shape != t.shape:
+            raise ValueError("%s: head_dim, or the shape of its output, differs" % name)
+        args.append((t.data_ptr(), stride, t.shape[1], o.data_ptr(), _head_rows(o, name + "_out", dtype, dev, n)))
+    (qp, qs, hq, qo, qos), (kp, ks, hk, ko, kos) = args
+    if rope is not None and pos is None:
+        raise ValueError("a rotation needs positions")
+    rc = lib().dart_norm_rope(qp, qs, hq, kp, ks, hk, n, D, code, _vector(q_weight, "q_weight", D, dtype, dev),
+                              _vector(k_weight, "k_weight", D, dtype, dev), eps,
+                              rope.at(pos, n, dev) if rope is not None else None, qo, qos, ko, kos, dev.index,
+                              _stream(stream, dev))
+    if rc != DART_OK:
+        raise DartError(rc, "dart_norm_rope")
+    return out
+
+
+class PagedCache:
+    """A cache of keys and values in pages: two tensors [pages, heads, page_size, head_dim], the caller's.  A sequence's token
+    number s lies in page ``table[sequence, s // page_size]``."""
+
+    def __init__(self, k, v):
+        import torch
+
+        if not (k.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device
+                and k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v must be contiguous CUDA tensors [pages, heads, page_size, head_dim] of one type and device")
+        self.k, self.v = k, v
+        self._status = torch.zeros(4, dtype=torch.int32, device=k.device)
+        self._c = dart_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3], _dtype_code(k.dtype),
+                             k.device.index)
+
+    def _ints(self, t, name, shape=None):
+        import torch
+
+        if t is None:
+            return None
+        if not (t.dtype == torch.int32 and t.device == self.k.device and t.is_contiguous() and (shape is None or t.shape == shape)):
+            raise ValueError("%s must be contiguous int32%s on %s" % (name, " %s" % (tuple(shape),) if shape is not None else "", self.k.device))
+        return t.data_ptr()
+
+    def _table(self, t, name):
+        import torch
+
+        if not (t.dtype == torch.int32 and t.device == self.k.device and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)
+                and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+            raise ValueError("%s must be int32 [sequences, pages] on %s" % (name, self.k.device))
+        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+    def append(self, k, v, table, start=None, cu_rows=None, idx=None, S=0, pos=None, rope=None, k_weight=None, eps=1e-6, stream=None):
+        """Rows of keys and values [N, heads, D] behind the ``start`` tokens that each sequence already has.  ``cu_rows``
+        [sequences + 1]: ragged numbers of rows (None: equally many).  ``idx`` (a reduction's out_idx, flat or [B, S_out]): take row
+        b * S + idx[n] for packed row n.  The keys are normalised (``k_weight``) and rotated (``rope``, at ``pos`` or at the slots)
+        on the way."""
+        dev, dtype = self.k.device, self.k.dtype
+        _, heads, _, D = self.k.shape
+        ks, vs = _head_rows(k, "k", dtype, dev), _head_rows(v, "v", dtype, dev, k.shape[0])
+        n_seq, n = table.shape[0], k.shape[0] if idx is None else idx.numel()
+        if k.shape[1:] != (heads, D) or v.shape[1:] != (heads, D):
+            raise ValueError("k and v must have the cache's heads and head_dim")
+        if idx is not None and (S < 1 or k.shape[0] != n_seq * S):
+            raise ValueError("with idx, k and v hold S rows per sequence")
+        tp, ts = self._table(table, "table")
+        if pos is not None:
+            pos = pos.reshape(-1) if rope is not None and rope.axes == 1 else pos
+        rc = lib().dart_cache_append(self._c, k.data_ptr(), ks, v.data_ptr(), vs, n_seq, n, self._ints(cu_rows, "cu_rows", (n_seq + 1,)),
+                                     self._ints(idx, "idx"), S, tp, ts, self._ints(start, "start", (n_seq,)),
+                                     _vector(k_weight, "k_weight", D, dtype, dev), eps,
+                                     rope.at(pos, n, dev) if rope is not None else None, self._status.data_ptr(),
+                                     _stream(stream, dev))
+        if rc != DART_OK:
+            raise DartError(rc, "dart_cache_append")
+
+    def status(self) -> int:
+        """DART_OK, or what a kernel found wrong since the last reading (a page or an index out of range, a wait that gave up).
+        Waits for the device; reading clears it."""
+        import torch
+
+        torch.cuda.synchronize(self.k.device)
+        code = int(self._status[0].item())
+        if code:
+            self._status.zero_()
+        return code

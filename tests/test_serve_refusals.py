@@ -1,0 +1,93 @@
+"""What the entry points around the reduction refuse, on the host and before anything is launched.  CPU only: the pointers below
+are never read."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def dart():
+    from paper_2502_11494_b200 import build, dart as d
+
+    build.build_library()
+    return d
+
+
+A, B, C, D_ = 1 << 20, 1 << 24, 1 << 28, 1 << 29  # addresses far apart
+
+
+def _rope(dart, **kw):
+    r = dict(inv_freq=A, pos=A, pos_stride=64, rot_dim=64, interleaved=0, n_axes=1, section=(0, 0, 0))
+    r.update(kw)
+    return dart.dart_rope(r["inv_freq"], r["pos"], r["pos_stride"], r["rot_dim"], r["interleaved"], r["n_axes"],
+                          (ctypes.c_int32 * 3)(*r["section"]))
+
+
+def _norm_rope(dart, **kw):
+    a = dict(q=A, qs=512, hq=4, k=B, ks=256, hk=2, n=8, D=128, dtype=0, wq=None, wk=None, eps=1e-6, rope=None, qo=C, qos=512, ko=D_,
+             kos=256)
+    a.update(kw)
+    return dart.dart_norm_rope(a["q"], a["qs"], a["hq"], a["k"], a["ks"], a["hk"], a["n"], a["D"], a["dtype"], a["wq"], a["wk"], a["eps"],
+                               a["rope"], a["qo"], a["qos"], a["ko"], a["kos"], 0, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), 0), (dict(n=0, q=None), 0),
+    (dict(n=-1), -2), (dict(hq=0, hk=0), -2), (dict(hq=-1), -2), (dict(D=0), -2), (dict(D=12), -2), (dict(D=264), -2),
+    (dict(eps=-1.0), -2), (dict(eps=float("nan")), -2), (dict(eps=float("inf")), -2), (dict(qs=504), -2), (dict(qs=516), -2), (dict(kos=128), -2),
+    (dict(hq=65536), -2), (dict(dtype=2), -9), (dict(dtype=-1), -9),
+    (dict(q=None), -1), (dict(ko=None), -1),
+    (dict(q=A + 8), -3), (dict(ko=D_ + 2), -3), (dict(wq=A + 4), -3),
+    (dict(qo=A + 16), -4), (dict(qo=A, qos=1024), -4), (dict(qo=B), -4), (dict(ko=C), -4), (dict(ko=A), -4), (dict(qo=B + 1024), -4),
+])
+def test_norm_rope_refuses(dart, kw, code):
+    assert _norm_rope(dart, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(inv_freq=None), -1), (dict(pos=None), -1), (dict(rot_dim=8), -2), (dict(rot_dim=144), -2), (dict(rot_dim=-16), -2),
+    (dict(n_axes=4), -2), (dict(n_axes=-1), -2), (dict(n_axes=3, section=(8, 8, 8)), -2), (dict(n_axes=3, section=(40, 8, -16)), -2),
+    (dict(n_axes=2, section=(16, 16, 0), pos_stride=7), -2), (dict(inv_freq=A + 2), -3), (dict(pos=A + 4), -3),
+])
+def test_rotations_that_are_refused(dart, kw, code):
+    assert _norm_rope(dart, rope=_rope(dart, **kw)) == code
+
+
+def test_columns_of_one_buffer_are_no_overlap(dart):
+    """Queries and keys side by side in a projection's output, and the results side by side in another: only the device is missing."""
+    got = _norm_rope(dart, q=A, qs=1024, k=A + 2 * 512, ks=1024, qo=C, qos=1024, ko=C + 2 * 512, kos=1024)
+    assert got in (dart.DART_OK, dart.DART_ERR_CUDA) and got != dart.DART_ERR_ALIAS
+    in_place = _norm_rope(dart, q=A, qs=1024, k=A + 2 * 512, ks=1024, qo=A, qos=1024, ko=A + 2 * 512, kos=1024, n=8)
+    assert in_place != dart.DART_ERR_ALIAS
+    assert _norm_rope(dart, q=A, qs=1024, k=A + 2 * 504, ks=1024, qo=A, qos=1024, ko=C, kos=256) == dart.DART_ERR_ALIAS
+
+
+def _append(dart, cache=None, **kw):
+    c = dict(k=C, v=D_, n_pages=16, n_heads=2, page_size=16, head_dim=128, dtype=0, device=0)
+    c.update(cache or {})
+    a = dict(k=A, ks=256, v=B, vs=256, n_seq=2, n=8, cu=None, idx=None, S=0, table=A, ts=4, start=None, wk=None, eps=1e-6, rope=None, status=None)
+    a.update(kw)
+    return dart.dart_cache_append(dart.dart_cache(*c.values()), a["k"], a["ks"], a["v"], a["vs"], a["n_seq"], a["n"], a["cu"], a["idx"], a["S"],
+                                  a["table"], a["ts"], a["start"], a["wk"], a["eps"], a["rope"], a["status"], None)
+
+
+@pytest.mark.parametrize("cache,kw,code", [
+    ({}, dict(n=0), 0), ({}, dict(n=0, k=None), 0),
+    (dict(k=None), {}, -1), (dict(n_pages=0), {}, -2), (dict(n_heads=0), {}, -2), (dict(page_size=0), {}, -2), (dict(head_dim=100), {}, -2),
+    (dict(head_dim=264), {}, -2), (dict(dtype=5), {}, -9), (dict(k=C + 8), {}, -3),
+    ({}, dict(n=7), -2), ({}, dict(n=-2), -2), ({}, dict(n_seq=0), -2), ({}, dict(ts=0), -2), ({}, dict(idx=A, S=0), -2), ({}, dict(ks=248), -2),
+    ({}, dict(k=None), -1), ({}, dict(table=None), -1), ({}, dict(v=B + 4), -3), ({}, dict(table=A + 2), -3), ({}, dict(status=A + 1), -3),
+    ({}, dict(k=C + 4096), -4), ({}, dict(v=D_), -4), (dict(v=C + 1024), {}, -4),
+])
+def test_append_refuses(dart, cache, kw, code):
+    assert _append(dart, cache, **kw) == code
+
+
+def test_append_takes_slots_as_positions_on_one_axis_only(dart):
+    assert _append(dart, rope=_rope(dart, pos=None, n_axes=3, section=(16, 8, 8))) == dart.DART_ERR_NULL
+    assert dart.dart_cache_append(None, A, 256, B, 256, 1, 1, None, None, 0, A, 1, None, None, 0.0, None, None, None) == dart.DART_ERR_NULL
+
+
+def test_struct_layouts(dart):
+    assert ctypes.sizeof(dart.dart_rope) == 48 and dart.dart_rope.rot_dim.offset == 24 and dart.dart_rope.section.offset == 36
+    assert ctypes.sizeof(dart.dart_cache) == 40 and dart.dart_cache.n_pages.offset == 16
