@@ -424,6 +424,47 @@ int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, 
                       int n_rows, const int32_t *cu_rows, const int32_t *idx, int S, const int32_t *table, int table_stride,
                       const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, int32_t *status, void *stream);
 
+/*
+ * Attention over a paged cache.  Sequence b has the query rows cu_q[b] .. cu_q[b + 1] - 1 (n of them) and kv_len[b] tokens in its
+ * pages, the new ones among them; its row t sees own tokens j <= kv_len[b] - n + t.  With n_groups > 0 sequences cu_group[g] ..
+ * cu_group[g + 1] - 1 also share a prefix of prefix_len[g] tokens in the pages of prefix_table[g], all of which all their rows see; its keys and
+ * values are read for all of them at once.  (Many questions about one reduced image: the packed prompt is the prefix.)
+ *   out = sum_j softmax_j(scale q.k_j) v_j over the visible tokens, head h of the queries with head h / (n_q_heads / n_heads) of the
+ *   cache; rows that see nothing: out = 0, lse = -inf.  Rows of no sequence are left as they are.
+ * Scores, softmax sums and outputs are held in fp32; the softmax weights enter the second product in the cache's type.
+ */
+typedef struct {
+    const void *q;                /* [n_rows] rows of n_q_heads heads, of the cache's type, device, 16-byte aligned */
+    void *out;                    /* rows as q; must not share a byte with q, the cache or lse */
+    float *lse;                   /* [n_rows][n_q_heads] log of the sum of exponentials, device, or NULL */
+    int64_t q_stride, out_stride; /* values from row to row, multiples of 8 */
+    int32_t n_rows, n_q_heads;    /* n_q_heads a multiple of the cache's heads */
+    int32_t n_seq, n_groups;      /* n_groups 0: no prefixes */
+    const int32_t *cu_q;          /* [n_seq + 1] device, ascending, or NULL: one row per sequence (n_rows == n_seq) */
+    const int32_t *table;         /* [n_seq][table_stride] device; entries behind a sequence's last page are not read */
+    const int32_t *kv_len;        /* [n_seq] device */
+    const int32_t *cu_group;      /* [n_groups + 1] device, ascending; sequences outside [cu_group[0], cu_group[n_groups]) have no prefix */
+    const int32_t *prefix_table;  /* [n_groups][prefix_stride] device */
+    const int32_t *prefix_len;    /* [n_groups] device */
+    int32_t table_stride, prefix_stride;
+    float scale;                  /* > 0 */
+    int32_t wait_limit;           /* 0: default (2 s); > 0: time limit in microseconds of every bounded device-side wait */
+    int32_t *status;              /* [4] device, or NULL.  status[0] becomes DART_ERR_CHECK where a page of a visible token is outside the
+                                     cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
+                                     do not ascend (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid) */
+} dart_attend_args;
+
+/*
+ * The call needs dart_attend_workspace(cache, args) bytes of device memory, 256-byte aligned, whose contents do not matter before or after
+ * it; calls that may overlap (other streams, captured graphs) need one each.  The size depends on sizes only, not on
+ * lengths; 0 for arguments that dart_attend refuses and for n_rows 0 (which does nothing).
+ * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, else UNSUPPORTED; fewer than 2^30 (row, head) pairs and 2^31 cached (head, token)
+ * pairs.  Keys and values of visible tokens must be finite; whatever else lies in the pages has no influence.
+ * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED, NOMEM (workspace too small), CUDA.
+ */
+size_t dart_attend_workspace(const dart_cache *cache, const dart_attend_args *args);
+int dart_attend(const dart_cache *cache, const dart_attend_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
 const char *dart_strerror(int code);
 int dart_version(void);
 

@@ -1,0 +1,692 @@
+// Attention over a paged cache of keys and values, with prefixes that groups of sequences share.
+//
+// Row t of a sequence with n query rows and L cached tokens of its own sees its group's whole prefix and own tokens
+// j <= L - n + t:  out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  s_j = scale q.k_j,  m a running maximum.
+//
+// Work.  The R = Hq / Hk query heads that share a KV head are rows of one product: row r = t R + (h mod R).  A segment is a
+// prefix (with the rows of all its group's sequences) or a sequence's own tokens (with its rows).  An ITEM is one KV head and one
+// tile of kM rows of a segment; its KV tokens are cut into TILES.  All tiles of all items stand in one line, and every
+// worker takes an equal, contiguous share of it: no worker waits for another, and one long sequence fills the GPU as well
+// as many short ones.  A prefix is read once per kM rows of its whole group.  The lengths are only known on the device; every
+// CTA adds them up itself (a launch for it would cost more).
+// Joining.  An item that one worker held whole, with nothing else to join, is written at once.  A worker's first and last item may
+// be shared with its neighbours: those pieces (not normalised sum, maximum, sum of exponentials, all in fp32) go to two places per
+// worker, and a second small launch joins them, always in the same order.  Items with a prefix to join leave theirs by row.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "dart_common.cuh"
+
+namespace dart {
+namespace attend {
+
+constexpr int kErrCheck = -8;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Partial results by row and head: [rows][Hq][D] and [rows][Hq] (maximum in log2 units, sum).
+struct Whole {
+    float *o;
+    float2 *ml;
+};
+
+// What one launch leaves for the joining one.
+struct Pieces {
+    int *item_base;  // [segments + 1] first item of every segment; the last: how many items, or -1: lengths that cannot be
+    int2 *items;     // first and last worker of every item
+    float *o;        // [workers][2][kM][D]: a worker's first piece, and its last one where the item goes on at the next worker
+    float2 *ml;      // [workers][2][kM]
+    int M;           // rows of a tile
+};
+
+struct Params {
+    const char *q;
+    char *out;
+    float *lse;
+    long long q_stride, out_stride; // bytes
+    const char *k, *v;
+    int n_rows, Hq, Hk, R, n_seq, n_groups, n_pages, page_shift;
+    int table_stride, ptable_stride;
+    const int32_t *cu_q, *table, *kv_len, *cu_group, *ptable, *plen;
+    float scale_log2;               // scale / ln 2: exponentials are powers of two
+    int32_t *status;                // 4 words
+    int n_prefix, n_own;            // segments of this launch: prefixes first
+    int n_workers, min_tiles, max_items;
+    Pieces pieces;
+    Whole whole[2];                 // [0] prefixes, [1] own tokens
+};
+
+struct Seg {
+    int row0, n_q, len, nmb, width;
+    const int32_t *table;
+    bool prefix;
+};
+
+__device__ __forceinline__ int clamp(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// First packed row of sequence b.  (Offsets that do not ascend are held inside the rows: nothing out of bounds is touched.)
+__device__ __forceinline__ int first_row(const Params &p, int b) { return p.cu_q ? clamp(p.cu_q[b], 0, p.n_rows) : b; }
+
+template <int kM>
+__device__ Seg load_seg(const Params &p, int s)
+{
+    Seg g;
+    int b0, b1;
+    g.prefix = s < p.n_prefix;
+    if (g.prefix) {
+        b0 = clamp(p.cu_group[s], 0, p.n_seq), b1 = clamp(p.cu_group[s + 1], b0, p.n_seq);
+        g.table = p.ptable + (long long)s * p.ptable_stride, g.width = p.ptable_stride, g.len = p.plen[s];
+    } else {
+        b0 = s - p.n_prefix, b1 = b0 + 1;
+        g.table = p.table + (long long)b0 * p.table_stride, g.width = p.table_stride, g.len = p.kv_len[b0];
+    }
+    g.row0 = first_row(p, b0);
+    g.n_q = max(first_row(p, b1) - g.row0, 0);
+    const long long most = (long long)g.width << p.page_shift;
+    if (g.len < 0 || g.len > most) {
+        if (p.status) *p.status = kErrCheck;
+        g.len = g.len < 0 ? 0 : (int)most;
+    }
+    g.nmb = g.prefix && g.len == 0 ? 0 : (g.n_q * p.R + kM - 1) / kM;
+    return g;
+}
+
+// Own tokens that row t sees.
+__device__ __forceinline__ int sees(const Seg &g, int t) { return g.prefix ? g.len : clamp(g.len - g.n_q + t + 1, 0, g.len); }
+// ... and what the last row of a tile sees: how far its KV tiles go.  A sequence's rows have a tile even if they see nothing (it
+// writes their zeros).
+template <int kM>
+__device__ __forceinline__ int tile_sees(const Params &p, const Seg &g, int mb)
+{
+    return g.prefix ? g.len : sees(g, (min((mb + 1) * kM, g.n_q * p.R) - 1) / p.R);
+}
+template <int kM, int kTile>
+__device__ __forceinline__ int tiles_of(const Params &p, const Seg &g, int mb)
+{
+    return max(1, (tile_sees<kM>(p, g, mb) + kTile - 1) / kTile);
+}
+template <int kM, int kTile>
+__device__ long long tiles_per_head(const Params &p, const Seg &g)
+{
+    if (g.nmb == 0) return 0;
+    if (g.prefix) return (long long)g.nmb * tiles_of<kM, kTile>(p, g, 0);
+    long long n = 0;
+    for (int mb = 0; mb < g.nmb; ++mb) n += tiles_of<kM, kTile>(p, g, mb);
+    return n;
+}
+
+struct Start {
+    int seg, item_base;
+    long long off; // tiles of the segment before the worker's first
+};
+
+template <int kWorkers>
+struct PlanShared {
+    Start start[kWorkers];
+    long long tiles[32];
+    int items[32];
+    long long n_tiles;
+};
+
+// Every CTA finds where its workers begin.  Block-wide; ends with a barrier.
+template <int kM, int kTile, int kWorkers>
+__device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, n_seg = p.n_prefix + p.n_own;
+    const int per = (n_seg + nt - 1) / nt, s0 = min(tid * per, n_seg), s1 = min(s0 + per, n_seg);
+    int items = 0;
+    long long tiles = 0;
+    for (int s = s0; s < s1; ++s) {
+        const Seg g = load_seg<kM>(p, s);
+        items += p.Hk * g.nmb, tiles += p.Hk * tiles_per_head<kM, kTile>(p, g);
+    }
+    int i_sum = items;
+    long long t_sum = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, i_sum, o);
+        const long long b = __shfl_up_sync(0xffffffffu, t_sum, o);
+        if (lane >= o) i_sum += a, t_sum += b;
+    }
+    if (lane == 31) sh.items[warp] = i_sum, sh.tiles[warp] = t_sum;
+    __syncthreads();
+    int i_all = 0;
+    long long t_all = 0;
+    for (int w = 0; w < nt / 32; ++w) {
+        if (w == warp) i_sum += i_all, t_sum += t_all;
+        i_all += sh.items[w], t_all += sh.tiles[w];
+    }
+    int ib = i_sum - items;
+    long long tb = t_sum - tiles;
+    const bool ok = i_all <= p.max_items;
+    if (tid < kWorkers) sh.start[tid] = Start{0, 0, 0};
+    if (tid == 0) {
+        sh.n_tiles = ok ? t_all : 0;
+        if (!ok && p.status) *p.status = kErrCheck;
+    }
+    const int active = (int)min((long long)p.n_workers, max(1ll, t_all / p.min_tiles));
+    __syncthreads();
+    if (ok && t_all > 0)
+#pragma unroll 1
+        for (int i = 0; i < kWorkers; ++i) {
+            const long long w = (long long)blockIdx.x * kWorkers + i;
+            const long long at = t_all * w / active;
+            if (w >= active || at < tb || at >= tb + tiles) continue;
+            int base = ib;
+            long long first = tb;
+            for (int s = s0; s < s1; ++s) {
+                const Seg g = load_seg<kM>(p, s);
+                const long long n = p.Hk * tiles_per_head<kM, kTile>(p, g);
+                if (at < first + n) {
+                    sh.start[i] = Start{s, base, at - first};
+                    break;
+                }
+                first += n, base += p.Hk * g.nmb;
+            }
+        }
+    if (blockIdx.x == 0) {
+        for (int s = s0; s < s1; ++s) {
+            p.pieces.item_base[s] = ib;
+            ib += p.Hk * load_seg<kM>(p, s).nmb;
+        }
+        if (tid == 0) p.pieces.item_base[n_seg] = ok ? i_all : -1;
+    }
+    __syncthreads();
+}
+
+// A worker's way through its share of the line, piece by piece.
+template <int kM, int kTile>
+struct Walk {
+    Seg g;
+    int s, item_base, hk, mb, a, b, nt, vis, worker; // piece: tiles [a, b) of nt
+    long long left;
+    bool done;
+
+    template <int kWorkers>
+    __device__ __forceinline__ void begin(const Params &p, const PlanShared<kWorkers> &sh, int local)
+    {
+        worker = blockIdx.x * kWorkers + local;
+        const int active = (int)min((long long)p.n_workers, max(1ll, sh.n_tiles / p.min_tiles));
+        left = worker < active ? sh.n_tiles * (worker + 1) / active - sh.n_tiles * worker / active : 0;
+        done = left == 0;
+        if (done) return;
+        const Start st = sh.start[local];
+        s = st.seg, item_base = st.item_base;
+        g = load_seg<kM>(p, s);
+        const long long head = tiles_per_head<kM, kTile>(p, g);
+        if (head <= 0) { // (lengths that change under the kernel)
+            done = true;
+            return;
+        }
+        hk = (int)(st.off / head), mb = 0;
+        long long off = st.off - hk * head;
+        for (; mb < g.nmb - 1; ++mb) {
+            nt = tiles_of<kM, kTile>(p, g, mb);
+            if (off < nt) break;
+            off -= nt;
+        }
+        a = (int)off;
+        piece(p);
+    }
+    __device__ __forceinline__ void piece(const Params &p)
+    {
+        vis = tile_sees<kM>(p, g, mb);
+        nt = tiles_of<kM, kTile>(p, g, mb);
+        b = (int)min((long long)nt, a + left);
+    }
+    __device__ __forceinline__ void next(const Params &p)
+    {
+        left -= max(1, b - a);
+        if (left <= 0) {
+            done = true;
+            return;
+        }
+        a = 0;
+        if (++mb == g.nmb) {
+            mb = 0;
+            if (++hk == p.Hk) {
+                hk = 0;
+                do {
+                    item_base += p.Hk * g.nmb;
+                    if (++s >= p.n_prefix + p.n_own) {
+                        done = true;
+                        return;
+                    }
+                    g = load_seg<kM>(p, s);
+                } while (g.nmb == 0);
+            }
+        }
+        piece(p);
+    }
+    __device__ __forceinline__ int item() const { return item_base + hk * g.nmb + mb; }
+    __device__ __forceinline__ bool is_whole() const { return a == 0 && b == nt; }
+    __device__ __forceinline__ long long place() const { return 2ll * worker + (a == 0); }
+    __device__ __forceinline__ void note(const Params &p) const // by one thread of the worker, once per piece
+    {
+        int *it = reinterpret_cast<int *>(p.pieces.items + item());
+        if (a == 0) it[0] = worker;
+        if (b == nt) it[1] = worker;
+    }
+};
+
+// ---- types --------------------------------------------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float exp2_approx(float x) // 2^x, within 2 ulp; 2^-inf = 0
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// log of the sum of exponentials, natural; -inf for rows that see nothing
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY; }
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+// Tiles of 16 rows: bound by the cache's bytes, not by products, so that mma.sync (16 x 8 x 16) is enough.  Every WARP is a worker
+// with a ring of its own in shared memory (cp.async, 16 bytes a lane; no barrier of the block, and nothing to merge between warps but
+// what the joining launch merges anyway).  Keys and values of 32 tokens take turns in the ring; with three places of 8 KB and eight
+// warps 128 KB are on their way per SM, which covers the latency of HBM at its full rate.  Tokens behind the end of a sequence
+// are filled with zeros in shared memory, whatever their page holds: 0 * NaN would be NaN.
+constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8;
+constexpr int kNarrowRing = 24576; // bytes of a warp's ring
+
+template <typename T>
+__device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_16816<__nv_bfloat16>(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma_16816<__half>(float *c, const uint32_t *a, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool kTrans>
+__device__ __forceinline__ void ldmatrix4(uint32_t *r, uint32_t addr)
+{
+    if (kTrans)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+// A worker's loads, in the order in which they are consumed: keys, then values, of tile after tile.
+template <int D>
+struct Feed {
+    Walk<kNarrowM, kNarrowTile> w;
+    int tile, pages, page_base; // tile at hand; lane l of `pages` holds table entry page_base + l
+    bool values;
+
+    __device__ __forceinline__ void fetch_pages(const Params &p, int from)
+    {
+        page_base = from;
+        const int i = from + (threadIdx.x & 31), need = (w.vis + (1 << p.page_shift) - 1) >> p.page_shift;
+        pages = -1;
+        if (i < need) {
+            pages = w.g.table[i];
+            if (pages < 0 || pages >= p.n_pages) {
+                pages = -1; // reads as zeros
+                if (p.status) *p.status = kErrCheck;
+            }
+        }
+    }
+    __device__ __forceinline__ void enter(const Params &p)
+    {
+        tile = w.a, values = false;
+        if (!w.done) fetch_pages(p, (tile * kNarrowTile) >> p.page_shift);
+    }
+    __device__ __forceinline__ void issue(const Params &p, uint32_t slot)
+    {
+        constexpr int kChunks = D / 8, kRowsPer = 32 / kChunks; // 16-byte chunks of a token; tokens per round of the warp
+        if (!w.done) {
+            const int lane = threadIdx.x & 31, tok0 = tile * kNarrowTile, chunk = lane % kChunks, mask = (1 << p.page_shift) - 1;
+            if (!values && ((tok0 + kNarrowTile - 1) >> p.page_shift) >= page_base + 32) fetch_pages(p, tok0 >> p.page_shift);
+            const char *base = values ? p.v : p.k;
+            const int pg0 = __shfl_sync(0xffffffffu, pages, (tok0 >> p.page_shift) - page_base);
+            const int pg1 = __shfl_sync(0xffffffffu, pages, ((tok0 + 16) >> p.page_shift) - page_base);
+#pragma unroll
+            for (int j = 0; j < kNarrowTile / kRowsPer; ++j) {
+                const int t = j * kRowsPer + lane / kChunks, pg = t < 16 ? pg0 : pg1;
+                const bool real = tok0 + t < w.vis && pg >= 0;
+                const long long row = (((long long)(real ? pg : 0) * p.Hk + w.hk) << p.page_shift) + ((tok0 + t) & mask);
+                const char *src = base + row * (D * 2) + chunk * 16;
+                const uint32_t dst = slot + t * (D * 2) + ((chunk ^ (t & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+            }
+            if (values && ++tile == w.b) {
+                w.next(p);
+                enter(p);
+            } else {
+                values = !values;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(const Params p)
+{
+    constexpr int kSlotBytes = kNarrowTile * D * 2, kSlots = kNarrowRing / kSlotBytes, kK = D / 16, kN = D / 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ PlanShared<kNarrowWarps> sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kNarrowRing;
+    wait_for_previous();
+    plan<kNarrowM, kNarrowTile, kNarrowWarps>(p, sh);
+
+    Walk<kNarrowM, kNarrowTile> w;
+    w.begin(p, sh, warp);
+    Feed<D> feed;
+    feed.w = w;
+    feed.enter(p);
+#pragma unroll 1
+    for (int i = 0; i < kSlots; ++i) feed.issue(p, ring + i * kSlotBytes);
+    int slot = 0;
+    // wait for the oldest load; afterwards its place is refilled
+    const auto arrived = [&]() {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
+        __syncwarp();
+        return ring + slot * kSlotBytes;
+    };
+    const auto refill = [&]() {
+        __syncwarp();
+        feed.issue(p, ring + slot * kSlotBytes);
+        slot = slot + 1 == kSlots ? 0 : slot + 1;
+    };
+
+    for (; !w.done; w.next(p)) {
+        const int rows = min(kNarrowM, w.g.n_q * p.R - w.mb * kNarrowM); // of this tile
+        const int r0 = lane >> 2, r1 = r0 + 8, c0 = (lane & 3) * 2;
+        // query fragments, and how many tokens the thread's two rows see
+        uint32_t qa[kK][4];
+        int lim[2];
+        long long row_at[2]; // row * Hq + head
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = w.mb * kNarrowM + (i ? r1 : r0);
+            const bool real = (i ? r1 : r0) < rows;
+            const int t = real ? r / p.R : 0, h = w.hk * p.R + (real ? r - t * p.R : 0);
+            lim[i] = real ? sees(w.g, t) : w.vis;
+            row_at[i] = (long long)(w.g.row0 + t) * p.Hq + h;
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(p.q + (long long)(w.g.row0 + t) * p.q_stride + (long long)h * (D * 2)) + (c0 >> 1);
+#pragma unroll
+            for (int kk = 0; kk < kK; ++kk) {
+                qa[kk][i] = real ? q[kk * 8] : 0u;
+                qa[kk][2 + i] = real ? q[kk * 8 + 4] : 0u;
+            }
+        }
+        float o[kN][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < kN; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+
+        for (int tile = w.a; tile < w.b; ++tile) {
+            // scores of 32 tokens: four products of 8 tokens, two fragments of keys per ldmatrix
+            uint32_t at = arrived();
+            float s[4][4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+            for (int kk = 0; kk < kK; ++kk)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const int t = n * 16 + ((lane >> 4) << 3) + (lane & 7), chunk = 2 * kk + ((lane >> 3) & 1);
+                    uint32_t b[4];
+                    ldmatrix4<false>(b, at + t * (D * 2) + ((chunk ^ (t & 7)) << 4));
+                    mma_16816<T>(s[2 * n], qa[kk], b[0], b[1]);
+                    mma_16816<T>(s[2 * n + 1], qa[kk], b[2], b[3]);
+                }
+            refill();
+            const int tok0 = tile * kNarrowTile + c0;
+            const bool masked = __any_sync(0xffffffffu, min(lim[0], lim[1]) < (tile + 1) * kNarrowTile);
+            float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][i] *= p.scale_log2;
+                    if (masked && tok0 + n * 8 + (i & 1) >= lim[i >> 1]) s[n][i] = -INFINITY;
+                    top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
+                }
+            float fix[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                const float now = fmaxf(m[i], top[i]);
+                fix[i] = m[i] == now ? 1.0f : exp2_approx(m[i] - now); // (both -inf: 1)
+                m[i] = now;
+                top[i] = now == -INFINITY ? 0.0f : now;
+                l[i] *= fix[i];
+            }
+            uint32_t pa[2][4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][i] = exp2_approx(s[n][i] - top[i >> 1]);
+                    l[i >> 1] += s[n][i];
+                }
+                // (weights enter the second product in the cache's type: half a step of it, relative, per token)
+                pa[n >> 1][(n & 1) * 2] = pack2<T>(s[n][0], s[n][1]);
+                pa[n >> 1][(n & 1) * 2 + 1] = pack2<T>(s[n][2], s[n][3]);
+            }
+            if (__any_sync(0xffffffffu, fix[0] != 1.0f || fix[1] != 1.0f))
+#pragma unroll
+                for (int n = 0; n < kN; ++n) o[n][0] *= fix[0], o[n][1] *= fix[0], o[n][2] *= fix[1], o[n][3] *= fix[1];
+            at = arrived();
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int n = 0; n < kN / 2; ++n) {
+                    const int t = kk * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), chunk = 2 * n + (lane >> 4);
+                    uint32_t b[4];
+                    ldmatrix4<true>(b, at + t * (D * 2) + ((chunk ^ (t & 7)) << 4));
+                    mma_16816<T>(o[2 * n], pa[kk], b[0], b[1]);
+                    mma_16816<T>(o[2 * n + 1], pa[kk], b[2], b[3]);
+                }
+            refill();
+        }
+
+        if (lane == 0) w.note(p);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+            const int r = i ? r1 : r0;
+            if (r >= rows) continue;
+            if (w.is_whole() && p.n_groups == 0) {
+                const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
+                const long long n = row_at[i] / p.Hq, h = row_at[i] - n * p.Hq;
+                uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + n * p.out_stride + h * (D * 2)) + (c0 >> 1);
+#pragma unroll
+                for (int d = 0; d < kN; ++d) dst[d * 4] = pack2<T>(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
+                if (p.lse && (lane & 3) == 0) p.lse[row_at[i]] = lse_of(m[i], l[i]);
+            } else {
+                float *dst;
+                float2 *ml;
+                if (w.is_whole()) {
+                    const Whole &to = p.whole[w.g.prefix ? 0 : 1];
+                    dst = to.o + row_at[i] * D, ml = to.ml + row_at[i];
+                } else {
+                    const long long at = w.place() * kNarrowM + r;
+                    dst = p.pieces.o + at * D, ml = p.pieces.ml + at;
+                }
+#pragma unroll
+                for (int d = 0; d < kN; ++d) *reinterpret_cast<float2 *>(dst + d * 8 + c0) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
+                if ((lane & 3) == 0) *ml = make_float2(m[i], l[i]);
+            }
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// ---- joining ----------------------------------------------------------------------------------------------------------------
+struct JoinParams {
+    Params p;           // (row tables, outputs, whole)
+    Pieces from[2];     // [0] prefixes, [1] own tokens
+    int seg_off[2];     // first segment of the kind in its launch
+    int n_seg[2];       // segments of that launch
+};
+
+// The pieces of one row and head: first the prefix's, then its own.
+struct PieceList {
+    const float *o[2];
+    const float2 *ml[2];
+    long long step; // rows from one piece to the next of the same item
+    int n[2];
+};
+
+// kWarps warps join one (row, head): one where there are many rows, four where few rows have long lists of pieces.
+template <typename T, int D, int kWarps>
+__global__ void __launch_bounds__(128) attend_join_kernel(const JoinParams j)
+{
+    constexpr int kPer = D / 32; // values of a lane
+    __shared__ float s_o[4][D], s_ml[4][2];
+    const Params &p = j.p;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kWarps;
+    const long long id = (long long)blockIdx.x * (4 / kWarps) + warp / kWarps;
+    wait_for_previous();
+    bool here = id < (long long)p.n_rows * p.Hq;
+    const int n = here ? (int)(id / p.Hq) : 0, h = here ? (int)(id - (long long)n * p.Hq) : 0, hk = h / p.R;
+    int b = n;
+    if (here && p.cu_q) {
+        here = n >= p.cu_q[0] && n < p.cu_q[p.n_seq];
+        int lo = 0, hi = p.n_seq;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.cu_q[mid] <= n)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        b = lo;
+    }
+    const float *o_at[2] = {nullptr, nullptr};
+    const float2 *ml_at[2] = {nullptr, nullptr};
+    int cnt[2] = {0, 0}, c_first[2] = {0, 0}, row_in[2] = {0, 0};
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        int s = b, row0;
+        if (kind == 0) {
+            if (p.n_groups == 0 || !here) continue;
+            if (b < p.cu_group[0] || b >= p.cu_group[p.n_groups]) continue; // in no group
+            int lo = 0, hi = p.n_groups;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (p.cu_group[mid] <= b)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            s = lo;
+            if (p.plen[s] <= 0) continue;
+            row0 = first_row(p, clamp(p.cu_group[s], 0, p.n_seq));
+        } else {
+            row0 = first_row(p, b);
+        }
+        const Pieces &f = j.from[kind];
+        if (!here || f.item_base[j.n_seg[kind]] < 0) {
+            here = false;
+            continue;
+        }
+        const int seg = j.seg_off[kind] + s, base = f.item_base[seg], nmb = (f.item_base[seg + 1] - base) / p.Hk;
+        const int r = (n - row0) * p.R + (h - hk * p.R), mb = r / f.M;
+        if (r < 0 || mb >= nmb) { // (offsets that do not ascend)
+            here = false;
+            continue;
+        }
+        const int2 c = f.items[base + hk * nmb + mb];
+        if (c.x == c.y) {
+            if (p.n_groups == 0) {
+                here = false; // written already
+                continue;
+            }
+            cnt[kind] = 1, c_first[kind] = -1;
+            o_at[kind] = p.whole[kind].o + id * D, ml_at[kind] = p.whole[kind].ml + id;
+        } else {
+            cnt[kind] = c.y - c.x + 1, c_first[kind] = c.x, row_in[kind] = r - mb * f.M;
+        }
+    }
+    const int all = here ? cnt[0] + cnt[1] : 0;
+    const auto find = [&](int i, const float *&o, const float2 *&ml) {
+        const int kind = i < cnt[0] ? 0 : 1;
+        if (kind) i -= cnt[0];
+        if (c_first[kind] < 0) {
+            o = o_at[kind], ml = ml_at[kind];
+        } else { // the item's first piece is the last one of its worker, the others are the first ones of theirs
+            const long long at = (2ll * (c_first[kind] + i) + (i == 0)) * j.from[kind].M + row_in[kind];
+            o = j.from[kind].o + at * D, ml = j.from[kind].ml + at;
+        }
+    };
+    float top = -INFINITY;
+    for (int i = lane; i < all; i += 32) {
+        const float *o;
+        const float2 *ml;
+        find(i, o, ml);
+        const float2 v = *ml;
+        if (v.y > 0.0f) top = fmaxf(top, v.x);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float acc[kPer], sum = 0.0f;
+#pragma unroll
+    for (int d = 0; d < kPer; ++d) acc[d] = 0.0f;
+#pragma unroll 4
+    for (int i = part; i < all; i += kWarps) {
+        const float *o;
+        const float2 *ml;
+        find(i, o, ml);
+        const float2 v = *ml;
+        const float wgt = v.y > 0.0f ? exp2_approx(v.x - top) : 0.0f;
+        sum += v.y * wgt;
+        if (wgt > 0.0f) {
+            if (kPer == 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(o + lane * 4);
+                acc[0] += x.x * wgt, acc[1] += x.y * wgt, acc[2 % kPer] += x.z * wgt, acc[3 % kPer] += x.w * wgt;
+            } else {
+                const float2 x = *reinterpret_cast<const float2 *>(o + lane * 2);
+                acc[0] += x.x * wgt, acc[1] += x.y * wgt;
+            }
+        }
+    }
+    if (kWarps > 1) {
+#pragma unroll
+        for (int d = 0; d < kPer; ++d) s_o[warp][lane * kPer + d] = acc[d];
+        if (lane == 0) s_ml[warp][0] = sum;
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+#pragma unroll
+            for (int d = 0; d < kPer; ++d) acc[d] += s_o[warp + w][lane * kPer + d];
+            sum += s_ml[warp + w][0];
+        }
+    }
+    if (!here) return;
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + (long long)n * p.out_stride + (long long)h * (D * 2)) + lane * (kPer / 2);
+#pragma unroll
+    for (int d = 0; d < kPer / 2; ++d) dst[d] = pack2<T>(acc[2 * d] * inv, acc[2 * d + 1] * inv);
+    if (p.lse && lane == 0) p.lse[id] = lse_of(top, sum);
+}
+
+} // namespace attend
+} // namespace dart

@@ -4,6 +4,7 @@
 
 #include <math.h>
 
+#include "dart_attend.cuh"
 #include "dart_host.cuh"
 #include "dart_rows.cuh"
 
@@ -87,6 +88,134 @@ int check_cache(const dart_cache *c)
 
 size_t cache_bytes(const dart_cache *c) { return (size_t)c->n_pages * c->n_heads * c->page_size * c->head_dim * 2; }
 
+// ---- attention ---------------------------------------------------------------------------------------------------------------
+
+constexpr int kJoinWide = 4096; // (row, head) pairs up to which four warps join one
+
+struct Launch {
+    bool prefix, own;
+    int M, n_workers, max_items, n_seg;
+    size_t item_base, items, ml, o; // places in the workspace
+};
+struct Layout {
+    Launch launch[2];
+    int n;
+    size_t whole_o[2], whole_ml[2], bytes;
+};
+
+int sm_count_of(int device)
+{
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 148;
+    }
+    return n;
+}
+
+// The launches of a call and their places in the workspace: from the sizes alone, lengths are only known on the device.
+Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
+{
+    using namespace dart::attend;
+    Layout L = {};
+    const long long R = a->n_q_heads / c->n_heads;
+    L.n = 1;
+    L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = true;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    for (int i = 0; i < L.n; ++i) {
+        Launch &l = L.launch[i];
+        l.M = kNarrowM, l.n_workers = sms * kNarrowWarps;
+        l.n_seg = (l.prefix ? a->n_groups : 0) + (l.own ? a->n_seq : 0);
+        const long long more = a->n_rows * R / l.M; // a segment of n rows has at most 1 + n / M tiles
+        const long long items = c->n_heads * (l.n_seg + more * ((l.prefix ? 1 : 0) + (l.own ? 1 : 0)));
+        l.max_items = items < 2147483647ll ? (int)items : 2147483647;
+        l.item_base = take(sizeof(int) * ((size_t)l.n_seg + 1));
+        l.items = take(sizeof(int2) * (size_t)l.max_items);
+        l.ml = take(sizeof(float2) * 2 * l.n_workers * l.M);
+        l.o = take(sizeof(float) * 2 * l.n_workers * (size_t)l.M * c->head_dim);
+    }
+    for (int k = 0; k < 2 && a->n_groups > 0; ++k) {
+        L.whole_ml[k] = take(sizeof(float2) * (size_t)a->n_rows * a->n_q_heads);
+        L.whole_o[k] = take(sizeof(float) * (size_t)a->n_rows * a->n_q_heads * c->head_dim);
+    }
+    L.bytes = at;
+    return L;
+}
+
+int check_attend(const dart_cache *c, const dart_attend_args *a)
+{
+    int rc = check_cache(c);
+    if (rc != DART_OK) return rc;
+    if (!a) return DART_ERR_NULL;
+    if (c->head_dim != 64 && c->head_dim != 128) return DART_ERR_UNSUPPORTED;
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return DART_ERR_UNSUPPORTED;
+    if (a->n_rows < 0 || a->n_seq < 1 || a->n_groups < 0 || a->n_q_heads < 1 || a->n_q_heads % c->n_heads != 0 || a->table_stride < 1 ||
+        !(a->scale > 0.0f) || isinf(a->scale) || (!a->cu_q && a->n_rows != a->n_seq) || (a->n_groups > 0 && a->prefix_stride < 1) || a->wait_limit < 0)
+        return DART_ERR_BAD_SHAPE;
+    // row and token numbers, and a table row's tokens, are counted in 32 bits
+    if ((long long)a->n_rows * a->n_q_heads > 2147483647ll / 2 || (long long)c->n_pages * c->n_heads * c->page_size > 2147483647ll - 1024 ||
+        (long long)a->table_stride * c->page_size > 2147483647ll / 2 || (long long)a->prefix_stride * c->page_size > 2147483647ll / 2 ||
+        ((long long)a->n_seq + a->n_groups) * c->n_heads > 2147483647ll / 4)
+        return DART_ERR_BAD_SHAPE;
+    if (a->n_rows == 0) return DART_OK;
+    if (!a->q || !a->out || !a->table || !a->kv_len || (a->n_groups > 0 && (!a->cu_group || !a->prefix_table || !a->prefix_len))) return DART_ERR_NULL;
+    if (!head_rows_ok(a->n_q_heads, c->head_dim, a->q_stride, a->n_rows) || !head_rows_ok(a->n_q_heads, c->head_dim, a->out_stride, a->n_rows))
+        return DART_ERR_BAD_SHAPE;
+    if (misaligned(a->q, 16) || misaligned(a->out, 16) || misaligned(a->lse, 4) || misaligned(a->cu_q, 4) || misaligned(a->table, 4) ||
+        misaligned(a->kv_len, 4) || misaligned(a->cu_group, 4) || misaligned(a->prefix_table, 4) || misaligned(a->prefix_len, 4) || misaligned(a->status, 4))
+        return DART_ERR_ALIGN;
+    const size_t all = cache_bytes(c), row = 2 * (size_t)a->n_q_heads * c->head_dim;
+    const size_t ob = (size_t)(a->n_rows - 1) * 2 * a->out_stride + row, lb = sizeof(float) * (size_t)a->n_rows * a->n_q_heads;
+    if (overlaps(a->out, ob, c->k, all) || overlaps(a->out, ob, c->v, all) || overlaps(a->lse, lb, c->k, all) || overlaps(a->lse, lb, c->v, all) ||
+        rows_overlap(a->out, a->n_rows, 2 * a->out_stride, row, a->q, a->n_rows, 2 * a->q_stride, row) || overlaps(a->lse, lb, a->out, ob) ||
+        overlaps(a->lse, lb, a->q, (size_t)(a->n_rows - 1) * 2 * a->q_stride + row))
+        return DART_ERR_ALIAS;
+    return DART_OK;
+}
+
+template <typename T, int D>
+int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, const Layout &L, int sms, cudaStream_t st)
+{
+    using namespace dart::attend;
+    Params p = {};
+    p.q = (const char *)a->q, p.out = (char *)a->out, p.lse = a->lse, p.q_stride = 2 * a->q_stride, p.out_stride = 2 * a->out_stride;
+    p.k = (const char *)c->k, p.v = (const char *)c->v;
+    p.n_rows = a->n_rows, p.Hq = a->n_q_heads, p.Hk = c->n_heads, p.R = a->n_q_heads / c->n_heads, p.n_seq = a->n_seq, p.n_groups = a->n_groups;
+    p.n_pages = c->n_pages;
+    while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
+    p.table_stride = a->table_stride, p.ptable_stride = a->prefix_stride;
+    p.cu_q = a->cu_q, p.table = a->table, p.kv_len = a->kv_len, p.cu_group = a->cu_group, p.ptable = a->prefix_table, p.plen = a->prefix_len;
+    p.scale_log2 = a->scale * 1.44269504088896340736f, p.status = a->status;
+    for (int k = 0; k < 2; ++k) p.whole[k] = Whole{(float *)(ws + L.whole_o[k]), (float2 *)(ws + L.whole_ml[k])};
+    JoinParams j = {};
+    for (int i = 0; i < L.n; ++i) {
+        const Launch &l = L.launch[i];
+        p.n_prefix = l.prefix ? a->n_groups : 0, p.n_own = l.own ? a->n_seq : 0;
+        p.n_workers = l.n_workers, p.min_tiles = 1, p.max_items = l.max_items;
+        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), l.M};
+        for (int k = 0; k < 2; ++k)
+            if (k ? l.own : l.prefix) j.from[k] = p.pieces, j.seg_off[k] = k ? p.n_prefix : 0, j.n_seg[k] = l.n_seg;
+        const size_t smem = kNarrowRing * kNarrowWarps;
+        cudaError_t e = cudaFuncSetAttribute(attend_narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e == cudaSuccess) e = launch_next(attend_narrow_kernel<T, D>, dim3(sms), kNarrowWarps * 32, smem, st, p);
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            return DART_ERR_CUDA;
+        }
+    }
+    j.p = p;
+    const long long pairs = (long long)a->n_rows * a->n_q_heads;
+    const cudaError_t e = pairs <= kJoinWide ? launch_next(attend_join_kernel<T, D, 4>, dim3((unsigned)pairs), 128, 0, st, j)
+                                             : launch_next(attend_join_kernel<T, D, 1>, dim3((unsigned)((pairs + 3) / 4)), 128, 0, st, j);
+    const cudaError_t e2 = cudaGetLastError();
+    return e == cudaSuccess && e2 == cudaSuccess ? DART_OK : DART_ERR_CUDA;
+}
+
 } // namespace
 
 extern "C" {
@@ -163,6 +292,31 @@ int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, 
     p.n_seq = n_seq, p.per_seq = cu_rows ? 0 : n_rows / n_seq, p.S = S, p.table_stride = table_stride, p.page_size = cache->page_size;
     p.n_pages = cache->n_pages, p.cu = cu_rows, p.idx = idx, p.table = table, p.start = start, p.status = status;
     return cache->dtype == DART_BF16 ? launch_rows<__nv_bfloat16, true>(p, (cudaStream_t)stream) : launch_rows<__half, true>(p, (cudaStream_t)stream);
+}
+
+size_t dart_attend_workspace(const dart_cache *cache, const dart_attend_args *args)
+{
+    if (check_attend(cache, args) != DART_OK || args->n_rows == 0) return 0;
+    return attend_layout(cache, args, sm_count_of(cache->device)).bytes;
+}
+
+int dart_attend(const dart_cache *cache, const dart_attend_args *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_attend(cache, args);
+    if (rc != DART_OK) return rc;
+    if (args->n_rows == 0) return DART_OK;
+    if (!workspace) return DART_ERR_NULL;
+    if (misaligned(workspace, 256)) return DART_ERR_ALIGN;
+    const int sms = sm_count_of(cache->device);
+    const Layout L = attend_layout(cache, args, sms);
+    if (workspace_bytes < L.bytes) return DART_ERR_NOMEM;
+    DeviceGuard g(cache->device);
+    if (!g.ok) return DART_ERR_CUDA;
+    char *ws = (char *)workspace;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (cache->dtype == DART_BF16)
+        return cache->head_dim == 128 ? launch_attend<__nv_bfloat16, 128>(cache, args, ws, L, sms, st) : launch_attend<__nv_bfloat16, 64>(cache, args, ws, L, sms, st);
+    return cache->head_dim == 128 ? launch_attend<__half, 128>(cache, args, ws, L, sms, st) : launch_attend<__half, 64>(cache, args, ws, L, sms, st);
 }
 
 } // extern "C"

@@ -7,6 +7,7 @@ device memory and streams, nothing else).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -29,7 +30,7 @@ EXPORTS = (
     "dart_create", "dart_destroy", "dart_set_shape", "dart_reduce", "dart_reduce_ex", "dart_reduce_host",
     "dart_status", "dart_status_detail", "dart_last_cuda_error", "dart_workspace_bytes", "dart_launch_count",
     "dart_profile_enable", "dart_profile_read", "dart_strerror", "dart_version", "dart_pivots_static",
-    "dart_gather_rows", "dart_norm_rope", "dart_cache_append",
+    "dart_gather_rows", "dart_norm_rope", "dart_cache_append", "dart_attend_workspace", "dart_attend",
 )
 DART_STATIC_MAX_ROWS = 262144
 DART_BF16, DART_FP16 = 0, 1
@@ -67,6 +68,15 @@ class dart_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("n_heads", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("device", ctypes.c_int32)]
+
+
+class dart_attend_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("n_rows", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_seq", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("cu_q", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("cu_group", ctypes.c_void_p), ("prefix_table", ctypes.c_void_p),
+                ("prefix_len", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("prefix_stride", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("wait_limit", ctypes.c_int32), ("status", ctypes.c_void_p)]
 
 
 class DartError(RuntimeError):
@@ -111,6 +121,9 @@ def lib() -> ctypes.CDLL:
                                      vp, i64, i32, vp]
         L.dart_cache_append.argtypes = [ctypes.POINTER(dart_cache), vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i32, vp, vp, f32,
                                         ctypes.POINTER(dart_rope), vp, vp]
+        L.dart_attend_workspace.argtypes = [ctypes.POINTER(dart_cache), ctypes.POINTER(dart_attend_args)]
+        L.dart_attend_workspace.restype = ctypes.c_size_t
+        L.dart_attend.argtypes = [ctypes.POINTER(dart_cache), ctypes.POINTER(dart_attend_args), vp, ctypes.c_size_t, vp]
         L.dart_strerror.argtypes = [i32]
         L.dart_strerror.restype = ctypes.c_char_p
         L.dart_version.argtypes = []
@@ -181,6 +194,15 @@ def dart_cache_append(cache: Optional[dart_cache], k, k_stride, v, v_stride, n_s
     """Rows of keys and values into the pages of a cache (raw device pointers); see include/dart.h."""
     return lib().dart_cache_append(cache, k, k_stride, v, v_stride, n_seq, n_rows, cu_rows, idx, S, table, table_stride, start,
                                    k_weight, eps, rope, status, stream)
+
+
+def dart_attend_workspace(cache: Optional[dart_cache], args: Optional[dart_attend_args]) -> int:
+    return lib().dart_attend_workspace(cache, args)
+
+
+def dart_attend(cache: Optional[dart_cache], args: Optional[dart_attend_args], workspace, workspace_bytes, stream) -> int:
+    """Attention over a paged cache, with prefixes that groups of sequences share (raw device pointers); see include/dart.h."""
+    return lib().dart_attend(cache, args, workspace, workspace_bytes, stream)
 
 
 def dart_status(ctx) -> int:
@@ -455,6 +477,47 @@ class PagedCache:
                                      _stream(stream, dev))
         if rc != DART_OK:
             raise DartError(rc, "dart_cache_append")
+
+    def attend(self, q, table, kv_len, cu_q=None, prefix=None, scale=None, out=None, lse=None, wait_limit=0, stream=None):
+        """Attention of query rows [N, Hq, D] over the cached tokens of their sequences: ``kv_len`` own tokens in the pages of
+        ``table`` [sequences, pages], the rows' own new tokens the last of them, and with ``prefix`` = (table [groups, pages],
+        lengths [groups], cu_group [groups + 1]) the tokens that a group of sequences shares.  ``cu_q`` [sequences + 1]: ragged
+        numbers of rows (None: one row per sequence).  ``scale``: None for 1 / sqrt(D).  Returns ``out`` (made if None); ``lse``, a
+        fp32 tensor [N, Hq], is filled if given."""
+        import torch
+
+        dev, dtype, D = self.k.device, self.k.dtype, self.k.shape[3]
+        if q.shape[-1] != D:
+            raise ValueError("q must have the cache's head_dim")
+        qs = _head_rows(q, "q", dtype, dev)
+        n, Hq, _ = q.shape
+        n_seq = table.shape[0]
+        on = torch.cuda.current_stream(dev)
+        with torch.cuda.stream(stream) if stream is not None and stream != on else contextlib.nullcontext():
+            if out is None:
+                out = torch.empty((n, Hq, D), dtype=dtype, device=dev)
+            elif out.shape != q.shape:
+                raise ValueError("out must have q's shape")
+            if lse is not None and not (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous() and lse.device == dev):
+                raise ValueError("lse must be contiguous fp32 [rows, heads] on the rows' device")
+            tp, ts = self._table(table, "table")
+            groups, pp, ps, cg, pl = 0, None, 0, None, None
+            if prefix is not None:
+                groups = prefix[0].shape[0]
+                pp, ps = self._table(prefix[0], "prefix table")
+                pl, cg = self._ints(prefix[1], "prefix lengths", (groups,)), self._ints(prefix[2], "cu_group", (groups + 1,))
+            a = dart_attend_args(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, qs,
+                                 _head_rows(out, "out", dtype, dev, n), n, Hq, n_seq, groups, self._ints(cu_q, "cu_q", (n_seq + 1,)), tp,
+                                 self._ints(kv_len, "kv_len", (n_seq,)), cg, pp, pl, ts, ps, D ** -0.5 if scale is None else scale,
+                                 wait_limit, self._status.data_ptr())
+            L = lib()
+            # (made for this call on its stream: the allocator keeps it apart from other streams' and graphs' calls)
+            need = L.dart_attend_workspace(self._c, a)
+            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+            rc = L.dart_attend(self._c, a, ws.data_ptr() if ws is not None else None, need, (stream or on).cuda_stream)
+        if rc != DART_OK:
+            raise DartError(rc, "dart_attend")
+        return out
 
     def status(self) -> int:
         """DART_OK, or what a kernel found wrong since the last reading (a page or an index out of range, a wait that gave up).
