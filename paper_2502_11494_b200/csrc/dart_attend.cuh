@@ -36,7 +36,7 @@ struct Pieces {
     int2 *items;     // first and last worker of every item
     float *o;        // [workers][2][kM][D]: a worker's first piece, and its last one where the item goes on at the next worker
     float2 *ml;      // [workers][2][kM]
-    int M;           // rows of a tile
+    int M, n_workers; // rows of a tile
 };
 
 struct Params {
@@ -614,6 +614,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const JoinParams j)
             continue;
         }
         const int2 c = f.items[base + hk * nmb + mb];
+        if (c.x < 0 || c.y < c.x || c.y >= f.n_workers) { // (a worker that gave up left its items unnoted)
+            here = false;
+            continue;
+        }
         if (c.x == c.y) {
             if (p.n_groups == 0) {
                 here = false; // written already

@@ -1,0 +1,480 @@
+// Attention over the paged cache for many rows: tiles of 128 rows on the tensor cores (see dart_attend.cuh for the work's division
+// and for how pieces are joined).
+//
+// A CTA has two ENGINES of a 128-row tile each: four softmax warps with a thread per
+// row, 256 columns of tensor memory; one thread issues tcgen05.mma for both.  For each KV tile of 128 tokens an engine does
+//   S = Q K^T   (Q and K in shared memory, 128-byte swizzle, S in tensor memory),
+//   P = 2^(S scale - m), in the cache's type, written over S,
+//   O += P V    (P from tensor memory, V as it lies in the cache: tokens along the product's inner dimension),
+// so that one engine's products run while the other one takes exponentials: 1024 cycles of the tensor pipe and 1024 of the
+// exponential unit a tile, the two that bound it.  O stays in tensor memory over a whole piece; it is only scaled when a
+// row's maximum has grown by more than 2^8 since it was last (fp32 sums and 16-bit weights lose nothing by a common factor).
+//   kPair false: the engines are two workers with a ring of tiles each (a place: keys or values of 128 tokens).
+//   kPair true:  they are one worker, 256 rows: both multiply with the same tiles.  Half the traffic from L2.
+// Rows behind a sequence's end come from its last page as they are; their scores are left out by selection, and the values among
+// the last 16 tokens of a product are set to zero in shared memory (0 * NaN would be NaN).
+// Every wait is bounded in time; a kernel that gives up says so in the status word, waits for its own copies and products, frees
+// the tensor memory and returns.
+#pragma once
+#include "dart_attend.cuh"
+#include "dart_ptx.cuh"
+
+namespace dart {
+namespace attend {
+
+using sweep::mbar_arrive;
+using sweep::mbar_arrive_expect_tx;
+using sweep::mbar_init;
+using sweep::smem_u32;
+using sweep::umma_commit;
+using sweep::umma_desc;
+
+constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384;
+constexpr int kHalf = 16384;                    // bytes: 128 tokens (or rows) x 64 columns
+constexpr int kWideSmem = 14 * kHalf + 1024;    // queries and the rings; the base is aligned to 1 KB
+constexpr int kMaxPlaces = 12;
+constexpr int kTmemCols = 512;
+// which wait gave up (status[1])
+enum { kWaitPlace = 110, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues };
+
+struct WideShared {
+    unsigned long long full[2][kMaxPlaces], empty[2][kMaxPlaces];
+    unsigned long long s_full[2], p_full[2], o_full[2], q_full[2], drain;
+    uint32_t tmem;
+    int abort;
+    PlanShared<2> plan;
+};
+
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(tm), "r"(x),
+                 "r"(y), "r"(bar)
+                 : "memory");
+}
+// D[128 x n] (+)= A[128 x 16] B[16 x n]; A and B of type T, D fp32.  b_mn: B's tokens run along the inner dimension (rows of 64 columns).
+template <typename T>
+constexpr uint32_t kFormat = 0; // fp16
+template <>
+constexpr uint32_t kFormat<__nv_bfloat16> = 1;
+template <typename T>
+__device__ __forceinline__ uint32_t wide_idesc(int n, bool b_mn)
+{
+    constexpr uint32_t fmt = kFormat<T>;
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kWideRows >> 4) << 24);
+}
+__device__ __forceinline__ void umma_ss(uint32_t d, unsigned long long a, unsigned long long b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, unsigned long long b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t at, float *v)
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+                 "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+                   "=r"(r[31])
+                 : "r"(at));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+                 "r"(r[15]), "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at));
+}
+
+// An engine's part of a piece: its rows, and how many of the piece's tiles its last row sees anything of.
+struct Share {
+    int rows, tiles;
+};
+template <int kM>
+__device__ __forceinline__ Share share_of(const Params &p, const Walk<kM, kWideTile> &w, int e)
+{
+    Share s;
+    const int r0 = w.mb * kM + (kM > kWideRows ? e * kWideRows : 0);
+    s.rows = clamp(w.g.n_q * p.R - r0, 0, kWideRows);
+    const int vis = s.rows == 0 ? 0 : sees(w.g, (r0 + s.rows - 1) / p.R);
+    s.tiles = max(0, min(w.b, (vis + kWideTile - 1) / kWideTile) - w.a);
+    return s;
+}
+
+template <typename T, int D, bool kPair>
+__global__ void __launch_bounds__(kWideThreads, 1)
+    attend_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params p, int *status,
+                       unsigned long long limit_cycles, int withhold)
+{
+    constexpr int kHalves = D / 64, kM = kPair ? 2 * kWideRows : kWideRows, kWorkers = kPair ? 1 : 2;
+    constexpr int kPlace = kHalves * kHalf;                              // bytes: the keys, or the values, of a tile
+    constexpr int kPlaces = (14 - 2 * kHalves) / kHalves / kWorkers; // of a ring
+    extern __shared__ unsigned char raw[];
+    __shared__ WideShared sh;
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const auto q_at = [&](int e) { return base + (uint32_t)e * kPlace; };
+    const auto place_at = [&](int ring, int i) { return base + (uint32_t)(2 + ring * kPlaces + i) * kPlace; };
+
+    if (threadIdx.x == 0) {
+        for (int r = 0; r < kWorkers; ++r)
+            for (int i = 0; i < kPlaces; ++i) {
+                mbar_init(smem_u32(&sh.full[r][i]), 1);
+                mbar_init(smem_u32(&sh.empty[r][i]), kPair ? 2 : 1);
+            }
+        for (int e = 0; e < 2; ++e) {
+            mbar_init(smem_u32(&sh.s_full[e]), 1);
+            mbar_init(smem_u32(&sh.p_full[e]), 4);
+            mbar_init(smem_u32(&sh.o_full[e]), 1);
+            mbar_init(smem_u32(&sh.q_full[e]), 4);
+        }
+        mbar_init(smem_u32(&sh.drain), 1);
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = sh.tmem;
+    wait_for_previous();
+    plan<kM, kWideTile, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
+    const PlanShared<kWorkers> &pl = *reinterpret_cast<const PlanShared<kWorkers> *>(&sh.plan);
+    const sweep::Ctl ctl{&sh.abort, status, limit_cycles};
+
+    // The softmax threads hold a row of 128 scores: 200 registers; the others give theirs (256 x 200 + 128 x 104 = 384 x 168).
+    if (warp >= 8)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    else
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+
+    if (warp >= 10) {
+        // ------------------------------------------------------------------ copies: one warp per ring, a lane per page
+        const int ring = warp - 10;
+        if (ring < kWorkers) {
+            Walk<kM, kWideTile> w;
+            w.begin(p, pl, ring);
+            const int box = min(1 << p.page_shift, kWideTile), nowhere = (p.n_pages * p.Hk) << p.page_shift;
+            uint32_t fills = 0;
+            bool ok = true;
+            for (; ok && !w.done; w.next(p)) {
+                const auto page_row = [&](int tile) { // where the lane's page of a tile begins among all rows of the cache
+                    const int tok = tile * kWideTile + lane * box;
+                    if (tile >= w.b || lane * box >= kWideTile || tok >= w.vis) return nowhere;
+                    const int pg = w.g.table[tok >> p.page_shift];
+                    if (pg < 0 || pg >= p.n_pages) {
+                        if (p.status) *p.status = kErrCheck;
+                        return nowhere; // reads as zeros
+                    }
+                    return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
+                };
+                int next_row = page_row(w.a);
+                for (int tile = w.a; ok && tile < w.b; ++tile) {
+                    const int row = next_row;
+                    next_row = page_row(tile + 1);
+                    const int n = (clamp(w.vis - tile * kWideTile, 0, kWideTile) + box - 1) / box;
+#pragma unroll 1
+                    for (int i = 0; ok && i < 2; ++i) {
+                        const int at = (int)(fills % kPlaces);
+                        const uint32_t bar = smem_u32(&sh.full[ring][at]);
+                        if (lane == 0) {
+                            ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, w.item());
+                            if (ok) mbar_arrive_expect_tx(bar, (uint32_t)(n * box * 128 * kHalves));
+                        }
+                        ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                        if (!ok) break;
+                        ++fills;
+                        if (lane < n)
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) tma_page(place_at(ring, at) + h * kHalf + lane * box * 128, i ? &tm_v : &tm_k, h * 64, row, bar);
+                    }
+                }
+            }
+            if (!ok && lane == 0) // a CTA does not end before its copies have landed
+                for (uint32_t i = 0; i < (uint32_t)kPlaces; ++i) {
+                    const uint32_t n = fills > i ? (fills - i - 1) / kPlaces + 1 : 0;
+                    if (n) ctl.wait_landed(smem_u32(&sh.full[ring][i]), (n - 1) & 1u);
+                }
+            __syncwarp();
+        }
+    } else if (warp >= 8) {
+        // ------------------------------------------------------------------ products: one thread for both engines
+        // (one queue for both: the engine whose products go first has its scores first, and the two stay half a tile apart.  With a
+        // thread per engine the tensor pipe takes turns between them, both wait for it and then both for the exponential unit: a
+        // tile took 8800 cycles.)
+        if (warp == 8 && lane == 0) {
+            const uint32_t id_s = wide_idesc<T>(kWideTile, false), id_o = wide_idesc<T>(D, true);
+            struct Engine {
+                Walk<kM, kWideTile> w;
+                Share s;
+                int tile;
+                uint32_t used, n_p, n_q;
+                bool values, asked; // at the second product; the piece's queries are there
+            } eng[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                Engine &g = eng[e];
+                g.w.begin(p, pl, kPair ? 0 : e);
+                g.used = g.n_p = g.n_q = 0, g.values = g.asked = false;
+                if (!g.w.done) g.s = share_of<kM>(p, g.w, e), g.tile = g.w.a;
+            }
+            // One product of an engine if what it needs is there.
+            const auto step = [&](Engine &g, int e) {
+                if (g.w.done) return false;
+                const int ring = kPair ? 0 : e, at = (int)(g.used % kPlaces);
+                const bool mine = g.tile < g.w.a + g.s.tiles;
+                const uint32_t s_at = tmem + e * 256, o_at = s_at + 128, empty = smem_u32(&sh.empty[ring][at]);
+                if (!g.values) {
+                    if (mine && !g.asked) {
+                        if (!sweep::mbar_test(smem_u32(&sh.q_full[e]), g.n_q & 1u)) return false;
+                        g.asked = true, ++g.n_q;
+                    }
+                    if (!sweep::mbar_test(smem_u32(&sh.full[ring][at]), (g.used / kPlaces) & 1u)) return false;
+                    if (mine) {
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const unsigned long long da = umma_desc(q_at(e)), db = umma_desc(place_at(ring, at));
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) { // (32 bytes on; a half further on after 64 columns)
+                            const int off = (kk >> 2) * (kHalf >> 4) + (kk & 3) * 2;
+                            umma_ss(s_at, da + off, db + off, id_s, kk != 0);
+                        }
+                        umma_commit(empty);
+                        umma_commit(smem_u32(&sh.s_full[e]));
+                    } else {
+                        mbar_arrive(empty);
+                    }
+                    g.values = true;
+                } else {
+                    if (mine && !sweep::mbar_test(smem_u32(&sh.p_full[e]), g.n_p & 1u)) return false;
+                    if (!sweep::mbar_test(smem_u32(&sh.full[ring][at]), (g.used / kPlaces) & 1u)) return false;
+                    if (mine) {
+                        ++g.n_p;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        // values as they lie: tokens along the inner dimension, a second half of columns 16 KB on
+                        const unsigned long long db = (umma_desc(place_at(ring, at)) & ~(0x3fffull << 16)) | (unsigned long long)(kHalf >> 4) << 16;
+                        const int steps = (min(g.w.vis - g.tile * kWideTile, kWideTile) + 15) >> 4;
+                        if (steps == 8) {
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk) umma_ts(o_at, s_at + kk * 8, db + kk * 128, id_o, g.tile > g.w.a || kk > 0);
+                        } else {
+                            for (int kk = 0; kk < steps; ++kk) // (16 tokens on: 2048 bytes; 8 columns of weights)
+                                umma_ts(o_at, s_at + kk * 8, db + kk * 128, id_o, g.tile > g.w.a || kk > 0);
+                        }
+                        umma_commit(empty);
+                    } else {
+                        mbar_arrive(empty);
+                    }
+                    g.values = false;
+                    if (++g.tile == g.w.b) {
+                        if (g.s.tiles > 0) umma_commit(smem_u32(&sh.o_full[e]));
+                        g.w.next(p);
+                        g.asked = false;
+                        if (!g.w.done) g.s = share_of<kM>(p, g.w, e), g.tile = g.w.a;
+                    }
+                }
+                ++g.used;
+                return true;
+            };
+            long long since = clock64();
+            bool ok = true;
+            for (uint32_t idle = 0; ok && !(eng[0].w.done && eng[1].w.done);) {
+                bool moved = false;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (step(eng[e], e)) {
+                        moved = true;
+                        step(eng[e], e); // behind a second product the next tile's first one
+                    }
+                if (moved) {
+                    idle = 0;
+                } else if ((++idle & 63u) == 1u) {
+                    if (idle == 1u)
+                        since = clock64();
+                    else if (ctl.aborted())
+                        ok = false;
+                    else if ((unsigned long long)(clock64() - since) > limit_cycles) {
+                        const Engine &g = eng[eng[0].w.done ? 1 : 0];
+                        ctl.give_up(g.values ? kWaitWeights : kWaitQueries, g.w.item());
+                        ok = false;
+                    }
+                }
+            }
+            if (!ok) {
+                umma_commit(smem_u32(&sh.drain));
+                ctl.wait_landed(smem_u32(&sh.drain), 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax: a thread per row
+        const int e = warp >> 2, ring = kPair ? 0 : e, row = (warp & 3) * 32 + lane;
+        const uint32_t s_at = tmem + e * 256 + ((uint32_t)((warp & 3) * 32) << 16), o_at = s_at + 128;
+        Walk<kM, kWideTile> w;
+        w.begin(p, pl, ring);
+        uint32_t seen = 0, n_s = 0, n_o = 0; // tiles of the ring passed so far; phases
+        bool ok = true;
+        for (; ok && !w.done; w.next(p)) {
+            const Share sr = share_of<kM>(p, w, e);
+            const int r = w.mb * kM + (kPair ? e * kWideRows : 0) + row;
+            const bool real = row < sr.rows;
+            const int t = real ? r / p.R : 0, h = w.hk * p.R + (real ? r - t * p.R : 0);
+            const int lim = real ? sees(w.g, t) : w.vis;
+            const long long row_at = (long long)(w.g.row0 + t) * p.Hq + h;
+            float m = -INFINITY, l = 0.0f;
+            if (sr.tiles > 0) {
+                // the row's queries, swizzled as a TMA copy would leave them (the piece before has ended with all its products)
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (long long)(w.g.row0 + t) * p.q_stride + (long long)h * (D * 2));
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 v = real ? src[c] : make_uint4(0, 0, 0, 0);
+                    const uint32_t dst = q_at(e) + (c >> 3) * kHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[e]));
+            }
+            for (int tile = w.a; ok && tile < w.a + sr.tiles; ++tile) {
+                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.s_full[e]), n_s & 1u, kWaitScores, w.item()));
+                if (!ok) break;
+                ++n_s;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                float s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(s_at + c * 32, s + c * 32);
+                tmem_wait_ld();
+                const int n_see = lim - tile * kWideTile;
+                if (__any_sync(0xffffffffu, n_see < kWideTile))
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = i < n_see ? s[i] : -INFINITY;
+                float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+#pragma unroll
+                for (int i = 4; i < 128; i += 4) t0 = fmaxf(t0, s[i]), t1 = fmaxf(t1, s[i + 1]), t2 = fmaxf(t2, s[i + 2]), t3 = fmaxf(t3, s[i + 3]);
+                const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * p.scale_log2;
+                const bool grown = top > m + 8.0f; // (from -inf: any)
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float now = fmaxf(m, top), fix = m == now ? 1.0f : exp2_approx(m - now);
+                    if (tile > w.a) { // (this tile's scores being there, the products before them have ended)
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_at + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fix);
+                            tmem_st16(o_at + c, o);
+                        }
+                    }
+                    l *= fix, m = now;
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;
+                float l0 = 0.0f, l1 = 0.0f, l2 = 0.0f, l3 = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w16[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float a = exp2_approx(fmaf(s[c * 32 + i], p.scale_log2, -ref)), b = exp2_approx(fmaf(s[c * 32 + i + 1], p.scale_log2, -ref));
+                        const float d = exp2_approx(fmaf(s[c * 32 + i + 2], p.scale_log2, -ref)), f = exp2_approx(fmaf(s[c * 32 + i + 3], p.scale_log2, -ref));
+                        l0 += a, l1 += b, l2 += d, l3 += f;
+                        // (weights enter the second product in the cache's type: half a step of it, relative, per token)
+                        w16[i / 2] = pack2<T>(a, b), w16[i / 2 + 1] = pack2<T>(d, f);
+                    }
+                    tmem_st16(s_at + c * 16, w16);
+                }
+                l += (l0 + l1) + (l2 + l3);
+                tmem_wait_st();
+                const int n_here = w.vis - tile * kWideTile; // tokens behind the last one: their values must be zeros up to the product's end
+                if (n_here < kWideTile && (n_here & 15)) {
+                    const uint32_t fill = (seen + (tile - w.a)) * 2 + 1;
+                    const int at = (int)(fill % kPlaces), n_zero = 16 - (n_here & 15);
+                    ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, w.item()));
+#pragma unroll
+                    for (int hh = 0; hh < kHalves; ++hh)
+                        if (ok && row < n_zero * 8)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(place_at(ring, at) + hh * kHalf + n_here * 128 + row * 16), "r"(0) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (!ok) break;
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0 && !(withhold && blockIdx.x == 0 && e == 0 && warp == 0)) mbar_arrive(smem_u32(&sh.p_full[e]));
+            }
+            seen += w.b - w.a;
+            if (sr.tiles > 0 && ok) {
+                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.o_full[e]), n_o & 1u, kWaitSums, w.item()));
+                ++n_o;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            }
+            if (!ok) break;
+            if (threadIdx.x == (kPair ? 0 : e * 128)) w.note(p);
+            const bool at_once = w.is_whole() && p.n_groups == 0;
+            const float inv = at_once && l > 0.0f ? 1.0f / l : 0.0f;
+            float *dst = nullptr;
+            if (!at_once && real) {
+                float2 *ml;
+                if (w.is_whole()) {
+                    const Whole &to = p.whole[w.g.prefix ? 0 : 1];
+                    dst = to.o + row_at * D, ml = to.ml + row_at;
+                } else {
+                    const long long at = w.place() * kM + (kPair ? e * kWideRows : 0) + row;
+                    dst = p.pieces.o + at * D, ml = p.pieces.ml + at;
+                }
+                *ml = make_float2(m, l);
+            }
+            if (at_once && real && p.lse) p.lse[row_at] = lse_of(m, l);
+            char *out = p.out + (long long)(w.g.row0 + t) * p.out_stride + (long long)h * (D * 2);
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                if (sr.tiles > 0) {
+                    tmem_ld32(o_at + c, o);
+                    tmem_wait_ld();
+                }
+                if (!real) continue;
+                if (at_once) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = l > 0.0f ? pack2<T>(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv) : 0u;
+                        *reinterpret_cast<uint4 *>(out + (c + i) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                } else if (sr.tiles > 0) { // (where l is 0 nobody reads them)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(dst + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+            }
+        }
+    }
+    // ---------------------------------------------------------------------- end
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+} // namespace attend
+} // namespace dart

@@ -4,7 +4,10 @@
 
 #include <math.h>
 
+#include <cuda.h>
+
 #include "dart_attend.cuh"
+#include "dart_attend_wide.cuh"
 #include "dart_host.cuh"
 #include "dart_rows.cuh"
 
@@ -92,16 +95,26 @@ size_t cache_bytes(const dart_cache *c) { return (size_t)c->n_pages * c->n_heads
 
 constexpr int kJoinWide = 4096; // (row, head) pairs up to which four warps join one
 
+enum Form { NARROW, WIDE, PAIR };
+
 struct Launch {
     bool prefix, own;
+    Form form;
     int M, n_workers, max_items, n_seg;
     size_t item_base, items, ml, o; // places in the workspace
 };
 struct Layout {
     Launch launch[2];
     int n;
-    size_t whole_o[2], whole_ml[2], bytes;
+    size_t whole_o[2], whole_ml[2], status, bytes;
 };
+
+// Rows of a tile by how many rows a segment has on average (the host knows the sizes, not the lengths).
+Form form_of(long long rows, long long segments)
+{
+    const long long avg = (rows + segments - 1) / segments;
+    return avg <= dart::attend::kNarrowM ? NARROW : avg <= dart::attend::kWideRows ? WIDE : PAIR;
+}
 
 int sm_count_of(int device)
 {
@@ -119,8 +132,10 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     using namespace dart::attend;
     Layout L = {};
     const long long R = a->n_q_heads / c->n_heads;
-    L.n = 1;
-    L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = true;
+    const Form own = form_of(a->n_rows * R, a->n_seq), shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups) : own;
+    L.n = own == shared ? 1 : 2;
+    L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = own == shared, L.launch[0].form = shared;
+    L.launch[1].own = true, L.launch[1].form = own;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -129,7 +144,8 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     };
     for (int i = 0; i < L.n; ++i) {
         Launch &l = L.launch[i];
-        l.M = kNarrowM, l.n_workers = sms * kNarrowWarps;
+        l.M = l.form == NARROW ? kNarrowM : l.form == WIDE ? kWideRows : 2 * kWideRows;
+        l.n_workers = sms * (l.form == NARROW ? kNarrowWarps : l.form == WIDE ? 2 : 1);
         l.n_seg = (l.prefix ? a->n_groups : 0) + (l.own ? a->n_seq : 0);
         const long long more = a->n_rows * R / l.M; // a segment of n rows has at most 1 + n / M tiles
         const long long items = c->n_heads * (l.n_seg + more * ((l.prefix ? 1 : 0) + (l.own ? 1 : 0)));
@@ -143,6 +159,7 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
         L.whole_ml[k] = take(sizeof(float2) * (size_t)a->n_rows * a->n_q_heads);
         L.whole_o[k] = take(sizeof(float) * (size_t)a->n_rows * a->n_q_heads * c->head_dim);
     }
+    L.status = take(16); // for callers without a status of their own
     L.bytes = at;
     return L;
 }
@@ -178,6 +195,37 @@ int check_attend(const dart_cache *c, const dart_attend_args *a)
     return DART_OK;
 }
 
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder()
+{
+    static const EncodeFn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+        return (EncodeFn)f;
+    }();
+    return fn;
+}
+
+// A cache as the rows of all its pages and heads; a box is a page (or 128 tokens of it) by 64 columns, swizzled.
+bool encode_cache(CUtensorMap *tm, const dart_cache *c, void *base)
+{
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->n_pages * c->n_heads * c->page_size}, strides[1] = {(cuuint64_t)c->head_dim * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)(c->page_size < dart::attend::kWideTile ? c->page_size : dart::attend::kWideTile)}, one[2] = {1, 1};
+    return fn(tm, c->dtype == DART_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename K>
+cudaError_t with_smem(K kernel, size_t smem)
+{
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
 template <typename T, int D>
 int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, const Layout &L, int sms, cudaStream_t st)
 {
@@ -193,16 +241,30 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     p.scale_log2 = a->scale * 1.44269504088896340736f, p.status = a->status;
     for (int k = 0; k < 2; ++k) p.whole[k] = Whole{(float *)(ws + L.whole_o[k]), (float2 *)(ws + L.whole_ml[k])};
     JoinParams j = {};
+    CUtensorMap tm_k, tm_v;
+    bool maps = false;
     for (int i = 0; i < L.n; ++i) {
         const Launch &l = L.launch[i];
         p.n_prefix = l.prefix ? a->n_groups : 0, p.n_own = l.own ? a->n_seq : 0;
         p.n_workers = l.n_workers, p.min_tiles = 1, p.max_items = l.max_items;
-        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), l.M};
+        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), l.M, l.n_workers};
         for (int k = 0; k < 2; ++k)
             if (k ? l.own : l.prefix) j.from[k] = p.pieces, j.seg_off[k] = k ? p.n_prefix : 0, j.n_seg[k] = l.n_seg;
-        const size_t smem = kNarrowRing * kNarrowWarps;
-        cudaError_t e = cudaFuncSetAttribute(attend_narrow_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e == cudaSuccess) e = launch_next(attend_narrow_kernel<T, D>, dim3(sms), kNarrowWarps * 32, smem, st, p);
+        cudaError_t e;
+        if (l.form == NARROW) {
+            const size_t smem = kNarrowRing * kNarrowWarps;
+            e = with_smem(attend_narrow_kernel<T, D>, smem);
+            if (e == cudaSuccess) e = launch_next(attend_narrow_kernel<T, D>, dim3(sms), kNarrowWarps * 32, smem, st, p);
+        } else {
+            if (!maps && (!encode_cache(&tm_k, c, c->k) || !encode_cache(&tm_v, c, c->v))) return DART_ERR_CUDA;
+            maps = true;
+            const auto kernel = l.form == PAIR ? attend_wide_kernel<T, D, true> : attend_wide_kernel<T, D, false>;
+            const unsigned long long limit = (a->wait_limit > 0 ? (unsigned long long)a->wait_limit : 2000000ull) * 2100ull;
+            e = with_smem(kernel, kWideSmem);
+            if (e == cudaSuccess)
+                e = launch_next(kernel, dim3(sms), kWideThreads, kWideSmem, st, tm_k, tm_v, p, a->status ? (int *)a->status : (int *)(ws + L.status), limit,
+                                a->test_withhold);
+        }
         if (e != cudaSuccess) {
             cudaGetLastError();
             return DART_ERR_CUDA;

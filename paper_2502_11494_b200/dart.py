@@ -76,7 +76,8 @@ class dart_attend_args(ctypes.Structure):
                 ("n_seq", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("cu_q", ctypes.c_void_p), ("table", ctypes.c_void_p),
                 ("kv_len", ctypes.c_void_p), ("cu_group", ctypes.c_void_p), ("prefix_table", ctypes.c_void_p),
                 ("prefix_len", ctypes.c_void_p), ("table_stride", ctypes.c_int32), ("prefix_stride", ctypes.c_int32),
-                ("scale", ctypes.c_float), ("wait_limit", ctypes.c_int32), ("status", ctypes.c_void_p)]
+                ("scale", ctypes.c_float), ("wait_limit", ctypes.c_int32), ("status", ctypes.c_void_p),
+                ("test_withhold", ctypes.c_int32)]
 
 
 class DartError(RuntimeError):
