@@ -35,16 +35,27 @@ constexpr int kWideSmem = 14 * kHalf + 1024;    // queries and the rings; the ba
 constexpr int kMaxPlaces = 12;
 constexpr int kTmemCols = 512;
 // which wait gave up (status[1])
-enum { kWaitPlace = 110, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues };
+enum { kWaitPlace = 110, kWaitKeys, kWaitValues, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues };
+
+// A place's note: whether engine e has work with the tile (bit e), whether it is the piece's first (8) and engine e's last of the piece
+// (bit 4 + e), how many 16-token steps its second product has (from bit 8); or that nothing follows.
+constexpr uint32_t kNoteFirst = 8, kNoteLast = 16, kNoteEnd = 1u << 31;
 
 struct WideShared {
     unsigned long long full[2][kMaxPlaces], empty[2][kMaxPlaces];
-    unsigned long long s_full[2], p_full[2], o_full[2], q_full[2], drain;
+    unsigned long long s_full[2], p_half[2], p_full[2], o_full[2], q_full[2], drain[2];
+    uint32_t note[2][kMaxPlaces]; // what a place holds (kNote*), for the thread that issues the products
     uint32_t tmem;
     int abort;
     PlanShared<2> plan;
 };
 
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(tm), "r"(x),
@@ -138,15 +149,16 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         for (int r = 0; r < kWorkers; ++r)
             for (int i = 0; i < kPlaces; ++i) {
                 mbar_init(smem_u32(&sh.full[r][i]), 1);
-                mbar_init(smem_u32(&sh.empty[r][i]), kPair ? 2 : 1);
+                mbar_init(smem_u32(&sh.empty[r][i]), 1);
             }
         for (int e = 0; e < 2; ++e) {
             mbar_init(smem_u32(&sh.s_full[e]), 1);
+            mbar_init(smem_u32(&sh.p_half[e]), 4);
             mbar_init(smem_u32(&sh.p_full[e]), 4);
             mbar_init(smem_u32(&sh.o_full[e]), 1);
+            mbar_init(smem_u32(&sh.drain[e]), 1);
             mbar_init(smem_u32(&sh.q_full[e]), 4);
         }
-        mbar_init(smem_u32(&sh.drain), 1);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -163,11 +175,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const PlanShared<kWorkers> &pl = *reinterpret_cast<const PlanShared<kWorkers> *>(&sh.plan);
     const sweep::Ctl ctl{&sh.abort, status, limit_cycles};
 
-    // The softmax threads hold a row of 128 scores: 200 registers; the others give theirs (256 x 200 + 128 x 104 = 384 x 168).
+    // The softmax threads hold a row of 128 scores: 216 registers; the others give theirs (256 x 216 + 128 x 72 = 384 x 168).
     if (warp >= 8)
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     else
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
 
     if (warp >= 10) {
         // ------------------------------------------------------------------ copies: one warp per ring, a lane per page
@@ -189,18 +201,24 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                     return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
                 };
+                const Share s0 = share_of<kM>(p, w, 0), s1 = kPair ? share_of<kM>(p, w, 1) : Share{0, 0};
                 int next_row = page_row(w.a);
                 for (int tile = w.a; ok && tile < w.b; ++tile) {
                     const int row = next_row;
                     next_row = page_row(tile + 1);
-                    const int n = (clamp(w.vis - tile * kWideTile, 0, kWideTile) + box - 1) / box;
+                    const int tokens = clamp(w.vis - tile * kWideTile, 0, kWideTile), n = (tokens + box - 1) / box, i_tile = tile - w.a;
+                    const uint32_t note = (i_tile < s0.tiles ? 1u : 0u) | (i_tile < s1.tiles ? 2u : 0u) | (i_tile == 0 ? kNoteFirst : 0u) |
+                                          (i_tile == s0.tiles - 1 ? kNoteLast : 0u) | (i_tile == s1.tiles - 1 ? 2 * kNoteLast : 0u) | (uint32_t)((tokens + 15) >> 4) << 8;
 #pragma unroll 1
                     for (int i = 0; ok && i < 2; ++i) {
                         const int at = (int)(fills % kPlaces);
                         const uint32_t bar = smem_u32(&sh.full[ring][at]);
                         if (lane == 0) {
                             ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, w.item());
-                            if (ok) mbar_arrive_expect_tx(bar, (uint32_t)(n * box * 128 * kHalves));
+                            if (ok) {
+                                sh.note[ring][at] = note;
+                                mbar_arrive_expect_tx(bar, (uint32_t)(n * box * 128 * kHalves));
+                            }
                         }
                         ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
                         if (!ok) break;
@@ -211,6 +229,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                 }
             }
+            if (ok && lane == 0) { // nothing follows
+                const int at = (int)(fills % kPlaces);
+                ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, -1);
+                if (ok) {
+                    sh.note[ring][at] = kNoteEnd;
+                    mbar_arrive(smem_u32(&sh.full[ring][at]));
+                }
+            }
             if (!ok && lane == 0) // a CTA does not end before its copies have landed
                 for (uint32_t i = 0; i < (uint32_t)kPlaces; ++i) {
                     const uint32_t n = fills > i ? (fills - i - 1) / kPlaces + 1 : 0;
@@ -219,113 +245,120 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             __syncwarp();
         }
     } else if (warp >= 8) {
-        // ------------------------------------------------------------------ products: one thread for both engines
-        // (one queue for both: the engine whose products go first has its scores first, and the two stay half a tile apart.  With a
-        // thread per engine the tensor pipe takes turns between them, both wait for it and then both for the exponential unit: a
-        // tile took 8800 cycles.)
-        if (warp == 8 && lane == 0) {
+        // ------------------------------------------------------------------ products
+        // The whole warp goes the same way, so that addresses stay in uniform registers; one lane issues.  (A lone thread that looks
+        // for the next product that is ready took 500 cycles from one batch to the next, a tile 7700.)
+        if (warp - 8 < kWorkers) {
+            const int ring = warp - 8;
             const uint32_t id_s = wide_idesc<T>(kWideTile, false), id_o = wide_idesc<T>(D, true);
-            struct Engine {
-                Walk<kM, kWideTile> w;
-                Share s;
-                int tile;
-                uint32_t used, n_p, n_q;
-                bool values, asked; // at the second product; the piece's queries are there
-            } eng[2];
+            const uint32_t full = smem_u32(&sh.full[ring][0]), empty = smem_u32(&sh.empty[ring][0]);
+            const unsigned long long desc = umma_desc(place_at(ring, 0)); // of the ring's first place; a place on: kPlace / 16 more
+            // values as they lie: tokens along the inner dimension, a second half of columns 16 KB on
+            const unsigned long long desc_v = (desc & ~(0x3fffull << 16)) | (unsigned long long)(kHalf >> 4) << 16;
+            const bool issues = elect_one();
+            const auto wait = [&](uint32_t bar, uint32_t phase, int where) {
+                if (__all_sync(0xffffffffu, sweep::mbar_try_wait(bar, phase))) return true;
+                return __all_sync(0xffffffffu, ctl.wait_bar(bar, phase, where, -1)) != 0;
+            };
+            uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};
+            const auto queries = [&](int e) { // a piece's queries are there
+                return wait(smem_u32(&sh.q_full[e]), n_q[e]++ & 1u, kWaitQueries);
+            };
+            const auto scores = [&](int e, int at) {
+                const unsigned long long da = umma_desc(q_at(e)), db = desc + (unsigned)(at * (kPlace >> 4));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issues) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                Engine &g = eng[e];
-                g.w.begin(p, pl, kPair ? 0 : e);
-                g.used = g.n_p = g.n_q = 0, g.values = g.asked = false;
-                if (!g.w.done) g.s = share_of<kM>(p, g.w, e), g.tile = g.w.a;
-            }
-            // One product of an engine if what it needs is there.
-            const auto step = [&](Engine &g, int e) {
-                if (g.w.done) return false;
-                const int ring = kPair ? 0 : e, at = (int)(g.used % kPlaces);
-                const bool mine = g.tile < g.w.a + g.s.tiles;
-                const uint32_t s_at = tmem + e * 256, o_at = s_at + 128, empty = smem_u32(&sh.empty[ring][at]);
-                if (!g.values) {
-                    if (mine && !g.asked) {
-                        if (!sweep::mbar_test(smem_u32(&sh.q_full[e]), g.n_q & 1u)) return false;
-                        g.asked = true, ++g.n_q;
+                    for (int kk = 0; kk < D / 16; ++kk) { // (32 bytes on; a half further on after 64 columns)
+                        const int off = (kk >> 2) * (kHalf >> 4) + (kk & 3) * 2;
+                        umma_ss(tmem + e * 256, da + off, db + off, id_s, kk != 0);
                     }
-                    if (!sweep::mbar_test(smem_u32(&sh.full[ring][at]), (g.used / kPlaces) & 1u)) return false;
-                    if (mine) {
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const unsigned long long da = umma_desc(q_at(e)), db = umma_desc(place_at(ring, at));
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) { // (32 bytes on; a half further on after 64 columns)
-                            const int off = (kk >> 2) * (kHalf >> 4) + (kk & 3) * 2;
-                            umma_ss(s_at, da + off, db + off, id_s, kk != 0);
-                        }
-                        umma_commit(empty);
-                        umma_commit(smem_u32(&sh.s_full[e]));
-                    } else {
-                        mbar_arrive(empty);
-                    }
-                    g.values = true;
-                } else {
-                    if (mine && !sweep::mbar_test(smem_u32(&sh.p_full[e]), g.n_p & 1u)) return false;
-                    if (!sweep::mbar_test(smem_u32(&sh.full[ring][at]), (g.used / kPlaces) & 1u)) return false;
-                    if (mine) {
-                        ++g.n_p;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        // values as they lie: tokens along the inner dimension, a second half of columns 16 KB on
-                        const unsigned long long db = (umma_desc(place_at(ring, at)) & ~(0x3fffull << 16)) | (unsigned long long)(kHalf >> 4) << 16;
-                        const int steps = (min(g.w.vis - g.tile * kWideTile, kWideTile) + 15) >> 4;
-                        if (steps == 8) {
-#pragma unroll
-                            for (int kk = 0; kk < 8; ++kk) umma_ts(o_at, s_at + kk * 8, db + kk * 128, id_o, g.tile > g.w.a || kk > 0);
-                        } else {
-                            for (int kk = 0; kk < steps; ++kk) // (16 tokens on: 2048 bytes; 8 columns of weights)
-                                umma_ts(o_at, s_at + kk * 8, db + kk * 128, id_o, g.tile > g.w.a || kk > 0);
-                        }
-                        umma_commit(empty);
-                    } else {
-                        mbar_arrive(empty);
-                    }
-                    g.values = false;
-                    if (++g.tile == g.w.b) {
-                        if (g.s.tiles > 0) umma_commit(smem_u32(&sh.o_full[e]));
-                        g.w.next(p);
-                        g.asked = false;
-                        if (!g.w.done) g.s = share_of<kM>(p, g.w, e), g.tile = g.w.a;
-                    }
+                    umma_commit(smem_u32(&sh.s_full[e]));
                 }
-                ++g.used;
+                __syncwarp();
+            };
+            const auto sums = [&](int e, int at, uint32_t note) { // in halves of 64 tokens, as their weights come
+                const unsigned long long db = desc_v + (unsigned)(at * (kPlace >> 4));
+                const int steps = (int)(note >> 8) & 15;
+                const uint32_t phase = n_p[e]++ & 1u, s_at = tmem + e * 256;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!wait(smem_u32(h ? &sh.p_full[e] : &sh.p_half[e]), phase, kWaitWeights)) return false;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (issues) {
+#pragma unroll
+                        for (int kk = h * 4; kk < h * 4 + 4; ++kk) // (16 tokens on: 2048 bytes; 8 columns of weights)
+                            if (kk < steps) umma_ts(s_at + 128, s_at + kk * 8, db + kk * 128, id_o, kk > 0 || !(note & kNoteFirst));
+                        if (h && (note & (kPair ? kNoteLast << e : kNoteLast))) umma_commit(smem_u32(&sh.o_full[e]));
+                    }
+                    __syncwarp();
+                }
                 return true;
             };
-            long long since = clock64();
+            const auto release = [&](int at) { // when all products so far have ended
+                if (issues) umma_commit(empty + at * 8);
+                __syncwarp();
+            };
+            int at = 0;
+            uint32_t round = 0;
             bool ok = true;
-            for (uint32_t idle = 0; ok && !(eng[0].w.done && eng[1].w.done);) {
-                bool moved = false;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (step(eng[e], e)) {
-                        moved = true;
-                        step(eng[e], e); // behind a second product the next tile's first one
-                    }
-                if (moved) {
-                    idle = 0;
-                } else if ((++idle & 63u) == 1u) {
-                    if (idle == 1u)
-                        since = clock64();
-                    else if (ctl.aborted())
-                        ok = false;
-                    else if ((unsigned long long)(clock64() - since) > limit_cycles) {
-                        const Engine &g = eng[eng[0].w.done ? 1 : 0];
-                        ctl.give_up(g.values ? kWaitWeights : kWaitQueries, g.w.item());
-                        ok = false;
-                    }
+            uint32_t note = 0;
+            const auto next_place = [&]() {
+                const int here = at;
+                if (++at == kPlaces) at = 0, round ^= 1u;
+                return here;
+            };
+            // keys of the first tile
+            ok = wait(full + at * 8, round, kWaitKeys);
+            if (ok) {
+                note = sh.note[ring][at];
+                if (!(note & kNoteEnd)) {
+                    for (int e = 0; ok && e < (kPair ? 2 : 1); ++e)
+                        if (note >> e & 1u) {
+                            ok = queries(ring + e);
+                            if (ok) scores(ring + e, at);
+                        }
+                    release(next_place());
                 }
             }
-            if (!ok) {
-                umma_commit(smem_u32(&sh.drain));
-                ctl.wait_landed(smem_u32(&sh.drain), 0);
+            while (ok && !(note & kNoteEnd)) {
+                // a tile's values, and the next one's keys: per engine the sums of the one, then the scores of the other, so that
+                // one engine's softmax runs beside the other one's products
+                ok = wait(full + at * 8, round, kWaitValues);
+                if (!ok) break;
+                const int at_v = next_place();
+                ok = wait(full + at * 8, round, kWaitKeys);
+                if (!ok) break;
+                const uint32_t next = sh.note[ring][at];
+                const bool fresh = (next & (kNoteFirst | kNoteEnd)) != 0; // a piece ends: the engines' sums are not held up by each other's end
+                if (kPair) {
+                    if (note & 1u) ok = sums(0, at_v, note);
+                    if (ok && !fresh && (next & 1u)) scores(0, at);
+                    if (ok && (note & 2u)) ok = sums(1, at_v, note);
+                    if (ok && !fresh && (next & 2u)) scores(1, at);
+                } else if (note & 1u) {
+                    ok = sums(ring, at_v, note);
+                    if (ok && !fresh && (next & 1u)) scores(ring, at);
+                }
+                if (!ok) break;
+                release(at_v);
+                note = next;
+                if (note & kNoteEnd) break;
+                if (fresh)
+                    for (int e = 0; ok && e < (kPair ? 2 : 1); ++e)
+                        if (note >> e & 1u) {
+                            ok = queries(ring + e);
+                            if (ok) scores(ring + e, at);
+                        }
+                if (!ok) break;
+                release(next_place());
             }
+            if (!ok && issues) {
+                umma_commit(smem_u32(&sh.drain[ring]));
+                ctl.wait_landed(smem_u32(&sh.drain[ring]), 0);
+            }
+            __syncwarp();
         }
-        __syncwarp();
     } else {
         // ------------------------------------------------------------------ softmax: a thread per row
         const int e = warp >> 2, ring = kPair ? 0 : e, row = (warp & 3) * 32 + lane;
@@ -369,12 +402,23 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 if (__any_sync(0xffffffffu, n_see < kWideTile))
 #pragma unroll
                     for (int i = 0; i < 128; ++i) s[i] = i < n_see ? s[i] : -INFINITY;
+                const int n_here = w.vis - tile * kWideTile; // tokens behind the last one: their values must be zeros up to the product's end
+                if (n_here < kWideTile && (n_here & 15)) {
+                    const uint32_t fill = (seen + (tile - w.a)) * 2 + 1;
+                    const int at = (int)(fill % kPlaces), n_zero = 16 - (n_here & 15);
+                    ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, w.item()));
+#pragma unroll
+                    for (int hh = 0; hh < kHalves; ++hh)
+                        if (ok && row < n_zero * 8)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(place_at(ring, at) + hh * kHalf + n_here * 128 + row * 16), "r"(0) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (!ok) break;
+                }
                 float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
 #pragma unroll
                 for (int i = 4; i < 128; i += 4) t0 = fmaxf(t0, s[i]), t1 = fmaxf(t1, s[i + 1]), t2 = fmaxf(t2, s[i + 2]), t3 = fmaxf(t3, s[i + 3]);
                 const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * p.scale_log2;
-                const bool grown = top > m + 8.0f; // (from -inf: any)
-                if (__any_sync(0xffffffffu, grown)) {
+                if (__any_sync(0xffffffffu, top > m + 8.0f)) { // (from -inf: any)
                     const float now = fmaxf(m, top), fix = m == now ? 1.0f : exp2_approx(m - now);
                     if (tile > w.a) { // (this tile's scores being there, the products before them have ended)
 #pragma unroll 1
@@ -389,38 +433,29 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                     l *= fix, m = now;
                 }
+                // Weights, in halves of 64 tokens so that the second product starts on the first while the other is made.
                 const float ref = m == -INFINITY ? 0.0f : m;
                 float l0 = 0.0f, l1 = 0.0f, l2 = 0.0f, l3 = 0.0f;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t w16[16];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float a = exp2_approx(fmaf(s[c * 32 + i], p.scale_log2, -ref)), b = exp2_approx(fmaf(s[c * 32 + i + 1], p.scale_log2, -ref));
-                        const float d = exp2_approx(fmaf(s[c * 32 + i + 2], p.scale_log2, -ref)), f = exp2_approx(fmaf(s[c * 32 + i + 3], p.scale_log2, -ref));
-                        l0 += a, l1 += b, l2 += d, l3 += f;
+                    for (int i = 0; i < 16; i += 2) {
+                        const float a0 = exp2_approx(fmaf(s[c * 32 + 2 * i], p.scale_log2, -ref)), a1 = exp2_approx(fmaf(s[c * 32 + 2 * i + 1], p.scale_log2, -ref));
+                        const float a2 = exp2_approx(fmaf(s[c * 32 + 2 * i + 2], p.scale_log2, -ref)), a3 = exp2_approx(fmaf(s[c * 32 + 2 * i + 3], p.scale_log2, -ref));
+                        l0 += a0, l1 += a1, l2 += a2, l3 += a3;
                         // (weights enter the second product in the cache's type: half a step of it, relative, per token)
-                        w16[i / 2] = pack2<T>(a, b), w16[i / 2 + 1] = pack2<T>(d, f);
+                        w16[i] = pack2<T>(a0, a1), w16[i + 1] = pack2<T>(a2, a3);
                     }
                     tmem_st16(s_at + c * 16, w16);
+                    if (c & 1) {
+                        tmem_wait_st();
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0 && !(withhold && blockIdx.x == 0 && warp == 0)) mbar_arrive(smem_u32(c == 1 ? &sh.p_half[e] : &sh.p_full[e]));
+                    }
                 }
                 l += (l0 + l1) + (l2 + l3);
-                tmem_wait_st();
-                const int n_here = w.vis - tile * kWideTile; // tokens behind the last one: their values must be zeros up to the product's end
-                if (n_here < kWideTile && (n_here & 15)) {
-                    const uint32_t fill = (seen + (tile - w.a)) * 2 + 1;
-                    const int at = (int)(fill % kPlaces), n_zero = 16 - (n_here & 15);
-                    ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, w.item()));
-#pragma unroll
-                    for (int hh = 0; hh < kHalves; ++hh)
-                        if (ok && row < n_zero * 8)
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(place_at(ring, at) + hh * kHalf + n_here * 128 + row * 16), "r"(0) : "memory");
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    if (!ok) break;
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0 && !(withhold && blockIdx.x == 0 && e == 0 && warp == 0)) mbar_arrive(smem_u32(&sh.p_full[e]));
             }
             seen += w.b - w.a;
             if (sr.tiles > 0 && ok) {
