@@ -5,8 +5,8 @@
 //
 // Work.  The R = Hq / Hk query heads that share a KV head are rows of one product: row r = t R + (h mod R).  A segment is a
 // prefix (with the rows of all its group's sequences) or a sequence's own tokens (with its rows).  An ITEM is one KV head and one
-// tile of kM rows of a segment; its KV tokens are cut into TILES.  All tiles of all items stand in one line, and every
-// worker takes an equal, contiguous share of it: no worker waits for another, and one long sequence fills the GPU as well
+// tile of kM rows of a segment; its KV tokens are cut into TILES.  All tiles of all items stand in one line, each item with kCost
+// tiles' worth of room before it (what beginning and ending a piece takes), and every worker takes an equal, contiguous share of it: no worker waits for another, and one long sequence fills the GPU as well
 // as many short ones.  A prefix is read once per kM rows of its whole group.  The lengths are only known on the device; every
 // CTA adds them up itself (a launch for it would cost more).
 // Joining.  An item that one worker held whole, with nothing else to join, is written at once.  A worker's first and last item may
@@ -105,19 +105,20 @@ __device__ __forceinline__ int tiles_of(const Params &p, const Seg &g, int mb)
 {
     return max(1, (tile_sees<kM>(p, g, mb) + kTile - 1) / kTile);
 }
-template <int kM, int kTile>
-__device__ long long tiles_per_head(const Params &p, const Seg &g)
+// A segment's part of the line, for one KV head.
+template <int kM, int kTile, int kCost>
+__device__ long long room_per_head(const Params &p, const Seg &g)
 {
     if (g.nmb == 0) return 0;
-    if (g.prefix) return (long long)g.nmb * tiles_of<kM, kTile>(p, g, 0);
+    if (g.prefix || g.nmb == 1) return (long long)g.nmb * (kCost + tiles_of<kM, kTile>(p, g, 0));
     long long n = 0;
-    for (int mb = 0; mb < g.nmb; ++mb) n += tiles_of<kM, kTile>(p, g, mb);
+    for (int mb = 0; mb < g.nmb; ++mb) n += kCost + tiles_of<kM, kTile>(p, g, mb);
     return n;
 }
 
 struct Start {
     int seg, item_base;
-    long long off; // tiles of the segment before the worker's first
+    long long off; // of the segment's room before the worker's share
 };
 
 template <int kWorkers>
@@ -129,7 +130,7 @@ struct PlanShared {
 };
 
 // Every CTA finds where its workers begin.  Block-wide; ends with a barrier.
-template <int kM, int kTile, int kWorkers>
+template <int kM, int kTile, int kCost, int kWorkers>
 __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, n_seg = p.n_prefix + p.n_own;
@@ -138,7 +139,7 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
     long long tiles = 0;
     for (int s = s0; s < s1; ++s) {
         const Seg g = load_seg<kM>(p, s);
-        items += p.Hk * g.nmb, tiles += p.Hk * tiles_per_head<kM, kTile>(p, g);
+        items += p.Hk * g.nmb, tiles += p.Hk * room_per_head<kM, kTile, kCost>(p, g);
     }
     int i_sum = items;
     long long t_sum = tiles;
@@ -176,7 +177,7 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
             long long first = tb;
             for (int s = s0; s < s1; ++s) {
                 const Seg g = load_seg<kM>(p, s);
-                const long long n = p.Hk * tiles_per_head<kM, kTile>(p, g);
+                const long long n = p.Hk * room_per_head<kM, kTile, kCost>(p, g);
                 if (at < first + n) {
                     sh.start[i] = Start{s, base, at - first};
                     break;
@@ -195,10 +196,11 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
 }
 
 // A worker's way through its share of the line, piece by piece.
-template <int kM, int kTile>
+template <int kM, int kTile, int kCost>
 struct Walk {
     Seg g;
     int s, item_base, hk, mb, a, b, nt, vis, worker; // piece: tiles [a, b) of nt
+    int from, to;                                    // ... and its place in the item's room
     long long left;
     bool done;
 
@@ -213,7 +215,7 @@ struct Walk {
         const Start st = sh.start[local];
         s = st.seg, item_base = st.item_base;
         g = load_seg<kM>(p, s);
-        const long long head = tiles_per_head<kM, kTile>(p, g);
+        const long long head = room_per_head<kM, kTile, kCost>(p, g);
         if (head <= 0) { // (lengths that change under the kernel)
             done = true;
             return;
@@ -221,42 +223,46 @@ struct Walk {
         hk = (int)(st.off / head), mb = 0;
         long long off = st.off - hk * head;
         for (; mb < g.nmb - 1; ++mb) {
-            nt = tiles_of<kM, kTile>(p, g, mb);
+            nt = kCost + tiles_of<kM, kTile>(p, g, mb);
             if (off < nt) break;
             off -= nt;
         }
-        a = (int)off;
+        from = (int)off;
         piece(p);
+        if (a == b) next(p); // (a share that ends before the item's first tile)
     }
     __device__ __forceinline__ void piece(const Params &p)
     {
         vis = tile_sees<kM>(p, g, mb);
         nt = tiles_of<kM, kTile>(p, g, mb);
-        b = (int)min((long long)nt, a + left);
+        to = (int)min((long long)nt + kCost, from + left);
+        a = max(0, from - kCost), b = max(0, to - kCost);
     }
     __device__ __forceinline__ void next(const Params &p)
     {
-        left -= max(1, b - a);
-        if (left <= 0) {
-            done = true;
-            return;
-        }
-        a = 0;
-        if (++mb == g.nmb) {
-            mb = 0;
-            if (++hk == p.Hk) {
-                hk = 0;
-                do {
-                    item_base += p.Hk * g.nmb;
-                    if (++s >= p.n_prefix + p.n_own) {
-                        done = true;
-                        return;
-                    }
-                    g = load_seg<kM>(p, s);
-                } while (g.nmb == 0);
+        do {
+            left -= max(1, to - from);
+            if (left <= 0) {
+                done = true;
+                return;
             }
-        }
-        piece(p);
+            from = 0;
+            if (++mb == g.nmb) {
+                mb = 0;
+                if (++hk == p.Hk) {
+                    hk = 0;
+                    do {
+                        item_base += p.Hk * g.nmb;
+                        if (++s >= p.n_prefix + p.n_own) {
+                            done = true;
+                            return;
+                        }
+                        g = load_seg<kM>(p, s);
+                    } while (g.nmb == 0);
+                }
+            }
+            piece(p);
+        } while (a == b);
     }
     __device__ __forceinline__ int item() const { return item_base + hk * g.nmb + mb; }
     __device__ __forceinline__ bool is_whole() const { return a == 0 && b == nt; }
@@ -299,7 +305,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? (m
 // what the joining launch merges anyway).  Keys and values of 32 tokens take turns in the ring; with three places of 8 KB and eight
 // warps 128 KB are on their way per SM, which covers the latency of HBM at its full rate.  Tokens behind the end of a sequence
 // are filled with zeros in shared memory, whatever their page holds: 0 * NaN would be NaN.
-constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8;
+constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8, kNarrowCost = 1;
 constexpr int kNarrowRing = 24576; // bytes of a warp's ring
 
 template <typename T>
@@ -330,7 +336,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t *r, uint32_t addr)
 // A worker's loads, in the order in which they are consumed: keys, then values, of tile after tile.
 template <int D>
 struct Feed {
-    Walk<kNarrowM, kNarrowTile> w;
+    Walk<kNarrowM, kNarrowTile, kNarrowCost> w;
     int tile, pages, page_base; // tile at hand; lane l of `pages` holds table entry page_base + l
     bool values;
 
@@ -390,9 +396,9 @@ __global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kNarrowRing;
     wait_for_previous();
-    plan<kNarrowM, kNarrowTile, kNarrowWarps>(p, sh);
+    plan<kNarrowM, kNarrowTile, kNarrowCost, kNarrowWarps>(p, sh);
 
-    Walk<kNarrowM, kNarrowTile> w;
+    Walk<kNarrowM, kNarrowTile, kNarrowCost> w;
     w.begin(p, sh, warp);
     Feed<D> feed;
     feed.w = w;

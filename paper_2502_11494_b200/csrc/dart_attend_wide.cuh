@@ -29,19 +29,30 @@ using sweep::smem_u32;
 using sweep::umma_commit;
 using sweep::umma_desc;
 
-constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384;
+constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384, kWideCost = 2;
+constexpr int kPieces = 4;                      // that may wait for the softmax threads
 constexpr int kHalf = 16384;                    // bytes: 128 tokens (or rows) x 64 columns
 constexpr int kWideSmem = 14 * kHalf + 1024;    // queries and the rings; the base is aligned to 1 KB
 constexpr int kMaxPlaces = 12;
 constexpr int kTmemCols = 512;
 // which wait gave up (status[1])
-enum { kWaitPlace = 110, kWaitKeys, kWaitValues, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues };
+enum { kWaitPlace = 110, kWaitKeys, kWaitValues, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues, kWaitPieces };
 
 // A place's note: whether engine e has work with the tile (bit e), whether it is the piece's first (8) and engine e's last of the piece
 // (bit 4 + e), how many 16-token steps its second product has (from bit 8); or that nothing follows.
 constexpr uint32_t kNoteFirst = 8, kNoteLast = 16, kNoteEnd = 1u << 31;
 
+// A piece as the softmax threads need it, written by the copying warp, which is ahead of them.
+struct PieceNote {
+    int row0, n_q, len, hk, r0; // its segment's rows and own tokens (prefix: all rows see all of them), its KV head, its first row
+    int a, b, vis, place;       // tiles; tokens that its last row sees; where its sums go: kToRows, or a place among the workers'
+    int prefix;                 // (b < 0: nothing follows)
+};
+constexpr int kToRows = -1;
+
 struct WideShared {
+    PieceNote piece[2][kPieces];
+    unsigned long long piece_full[2][kPieces], piece_empty[2][kPieces];
     unsigned long long full[2][kMaxPlaces], empty[2][kMaxPlaces];
     unsigned long long s_full[2], p_half[2], p_full[2], o_full[2], q_full[2], drain[2];
     uint32_t note[2][kMaxPlaces]; // what a place holds (kNote*), for the thread that issues the products
@@ -119,14 +130,15 @@ __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t *r)
 struct Share {
     int rows, tiles;
 };
+__device__ __forceinline__ int sees(const PieceNote &g, int t) { return g.prefix ? g.len : clamp(g.len - g.n_q + t + 1, 0, g.len); }
 template <int kM>
-__device__ __forceinline__ Share share_of(const Params &p, const Walk<kM, kWideTile> &w, int e)
+__device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, int e)
 {
     Share s;
-    const int r0 = w.mb * kM + (kM > kWideRows ? e * kWideRows : 0);
-    s.rows = clamp(w.g.n_q * p.R - r0, 0, kWideRows);
-    const int vis = s.rows == 0 ? 0 : sees(w.g, (r0 + s.rows - 1) / p.R);
-    s.tiles = max(0, min(w.b, (vis + kWideTile - 1) / kWideTile) - w.a);
+    const int r0 = g.r0 + (kM > kWideRows ? e * kWideRows : 0);
+    s.rows = clamp(g.n_q * p.R - r0, 0, kWideRows);
+    const int vis = s.rows == 0 ? 0 : sees(g, (r0 + s.rows - 1) / p.R);
+    s.tiles = max(0, min(g.b, (vis + kWideTile - 1) / kWideTile) - g.a);
     return s;
 }
 
@@ -146,6 +158,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     const auto place_at = [&](int ring, int i) { return base + (uint32_t)(2 + ring * kPlaces + i) * kPlace; };
 
     if (threadIdx.x == 0) {
+        for (int r = 0; r < kWorkers; ++r)
+            for (int i = 0; i < kPieces; ++i) {
+                mbar_init(smem_u32(&sh.piece_full[r][i]), 1);
+                mbar_init(smem_u32(&sh.piece_empty[r][i]), kPair ? 8 : 4);
+            }
         for (int r = 0; r < kWorkers; ++r)
             for (int i = 0; i < kPlaces; ++i) {
                 mbar_init(smem_u32(&sh.full[r][i]), 1);
@@ -171,7 +188,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh.tmem;
     wait_for_previous();
-    plan<kM, kWideTile, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
+    plan<kM, kWideTile, kWideCost, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
     const PlanShared<kWorkers> &pl = *reinterpret_cast<const PlanShared<kWorkers> *>(&sh.plan);
     const sweep::Ctl ctl{&sh.abort, status, limit_cycles};
 
@@ -185,12 +202,28 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ------------------------------------------------------------------ copies: one warp per ring, a lane per page
         const int ring = warp - 10;
         if (ring < kWorkers) {
-            Walk<kM, kWideTile> w;
+            Walk<kM, kWideTile, kWideCost> w;
             w.begin(p, pl, ring);
             const int box = min(1 << p.page_shift, kWideTile), nowhere = (p.n_pages * p.Hk) << p.page_shift;
-            uint32_t fills = 0;
+            uint32_t fills = 0, pieces = 0;
             bool ok = true;
+            const auto announce = [&](const PieceNote &note) { // to the softmax threads
+                const int at = (int)(pieces % kPieces);
+                if (lane == 0) {
+                    ok = ctl.wait_bar(smem_u32(&sh.piece_empty[ring][at]), ((pieces / kPieces) & 1u) ^ 1u, kWaitPieces, pieces);
+                    if (ok) {
+                        sh.piece[ring][at] = note;
+                        mbar_arrive(smem_u32(&sh.piece_full[ring][at]));
+                    }
+                }
+                ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                ++pieces;
+            };
             for (; ok && !w.done; w.next(p)) {
+                const PieceNote piece{w.g.row0, w.g.n_q, w.g.len, w.hk, w.mb * kM, w.a, w.b, w.vis, w.is_whole() ? kToRows : (int)w.place(), (int)w.g.prefix};
+                if (lane == 0) w.note(p);
+                announce(piece);
+                if (!ok) break;
                 const auto page_row = [&](int tile) { // where the lane's page of a tile begins among all rows of the cache
                     const int tok = tile * kWideTile + lane * box;
                     if (tile >= w.b || lane * box >= kWideTile || tok >= w.vis) return nowhere;
@@ -201,7 +234,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                     return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
                 };
-                const Share s0 = share_of<kM>(p, w, 0), s1 = kPair ? share_of<kM>(p, w, 1) : Share{0, 0};
+                const Share s0 = share_of<kM>(p, piece, 0), s1 = kPair ? share_of<kM>(p, piece, 1) : Share{0, 0};
                 int next_row = page_row(w.a);
                 for (int tile = w.a; ok && tile < w.b; ++tile) {
                     const int row = next_row;
@@ -229,6 +262,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                 }
             }
+            if (ok) announce(PieceNote{0, 0, 0, 0, 0, 0, -1, 0, 0, 0});
             if (ok && lane == 0) { // nothing follows
                 const int at = (int)(fills % kPlaces);
                 ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, -1);
@@ -363,26 +397,53 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ------------------------------------------------------------------ softmax: a thread per row
         const int e = warp >> 2, ring = kPair ? 0 : e, row = (warp & 3) * 32 + lane;
         const uint32_t s_at = tmem + e * 256 + ((uint32_t)((warp & 3) * 32) << 16), o_at = s_at + 128;
-        Walk<kM, kWideTile> w;
-        w.begin(p, pl, ring);
-        uint32_t seen = 0, n_s = 0, n_o = 0; // tiles of the ring passed so far; phases
+        const uint32_t stage = q_at(e) + (warp & 3) * 32 * 128; // the warp's rows of the queries (first half of their columns)
+        uint32_t seen = 0, n_s = 0, n_o = 0, pieces = 0; // tiles of the ring passed so far; phases
         bool ok = true;
-        for (; ok && !w.done; w.next(p)) {
-            const Share sr = share_of<kM>(p, w, e);
-            const int r = w.mb * kM + (kPair ? e * kWideRows : 0) + row;
-            const bool real = row < sr.rows;
-            const int t = real ? r / p.R : 0, h = w.hk * p.R + (real ? r - t * p.R : 0);
-            const int lim = real ? sees(w.g, t) : w.vis;
-            const long long row_at = (long long)(w.g.row0 + t) * p.Hq + h;
+        PieceNote w{0, 0, 0, 0, 0, 0, -1, 0, 0, 0};
+        Share sr{0, 0};
+        int n = 0, h = 0, lim = 0; // the thread's row: packed row and head; how many tokens it sees
+        bool real = false;
+        const auto next_piece = [&]() {
+            const int at = (int)(pieces % kPieces);
+            ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.piece_full[ring][at]), (pieces / kPieces) & 1u, kWaitPieces, pieces));
+            if (!ok) return;
+            w = sh.piece[ring][at];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.piece_empty[ring][at]));
+            ++pieces;
+            if (w.b < 0) return;
+            sr = share_of<kM>(p, w, e);
+            const int r = w.r0 + (kPair ? e * kWideRows : 0) + row;
+            real = row < sr.rows;
+            const int t = real ? r / p.R : 0;
+            n = w.row0 + t, h = w.hk * p.R + (real ? r - t * p.R : 0);
+            lim = real ? sees(w, t) : w.vis;
+        };
+        // Queries: 16 (8) lanes a row, so that a load takes whole lines.
+        constexpr int kRowLanes = D / 8, kRowsPer = 32 / kRowLanes;
+        uint4 q[kRowLanes];
+        const auto fetch_queries = [&]() { // (always all of q: nothing of the piece before stays in registers)
+            const bool any = w.b >= 0 && sr.tiles > 0;
+#pragma unroll
+            for (int i = 0; i < kRowLanes; ++i) {
+                const int from = i * kRowsPer + lane / kRowLanes;
+                const int qn = __shfl_sync(0xffffffffu, n, from), qh = __shfl_sync(0xffffffffu, h, from);
+                const bool there = __shfl_sync(0xffffffffu, (int)real, from) != 0;
+                q[i] = any && there ? *reinterpret_cast<const uint4 *>(p.q + (long long)qn * p.q_stride + (long long)qh * (D * 2) + (lane % kRowLanes) * 16) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        next_piece();
+        fetch_queries();
+        while (ok && w.b >= 0) {
             float m = -INFINITY, l = 0.0f;
             if (sr.tiles > 0) {
-                // the row's queries, swizzled as a TMA copy would leave them (the piece before has ended with all its products)
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (long long)(w.g.row0 + t) * p.q_stride + (long long)h * (D * 2));
+                // swizzled as a TMA copy would leave them (the piece before has ended with all its products)
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 v = real ? src[c] : make_uint4(0, 0, 0, 0);
-                    const uint32_t dst = q_at(e) + (c >> 3) * kHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                for (int i = 0; i < kRowLanes; ++i) {
+                    const int c = lane % kRowLanes, r = (warp & 3) * 32 + i * kRowsPer + lane / kRowLanes;
+                    const uint32_t dst = q_at(e) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(q[i].x), "r"(q[i].y), "r"(q[i].z), "r"(q[i].w) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -390,7 +451,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[e]));
             }
             for (int tile = w.a; ok && tile < w.a + sr.tiles; ++tile) {
-                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.s_full[e]), n_s & 1u, kWaitScores, w.item()));
+                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.s_full[e]), n_s & 1u, kWaitScores, pieces));
                 if (!ok) break;
                 ++n_s;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -406,7 +467,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 if (n_here < kWideTile && (n_here & 15)) {
                     const uint32_t fill = (seen + (tile - w.a)) * 2 + 1;
                     const int at = (int)(fill % kPlaces), n_zero = 16 - (n_here & 15);
-                    ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, w.item()));
+                    ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, pieces));
 #pragma unroll
                     for (int hh = 0; hh < kHalves; ++hh)
                         if (ok && row < n_zero * 8)
@@ -457,50 +518,72 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 }
                 l += (l0 + l1) + (l2 + l3);
             }
+            if (!ok) break;
             seen += w.b - w.a;
-            if (sr.tiles > 0 && ok) {
-                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.o_full[e]), n_o & 1u, kWaitSums, w.item()));
+            // what the piece leaves, and where; then, while its last products run, the next one's queries are asked for
+            const Share had = sr;
+            const bool at_once = w.place == kToRows && p.n_groups == 0, was_real = real;
+            const Whole &to = p.whole[w.prefix ? 0 : 1];
+            const int out_n = n, out_h = h;
+            const int dst_row = !real ? -1 : w.place == kToRows ? n * p.Hq + h : w.place * kM + (kPair ? e * kWideRows : 0) + row;
+            float *const dst = w.place == kToRows ? to.o : p.pieces.o;
+            if (was_real) {
+                if (!at_once)
+                    (w.place == kToRows ? to.ml : p.pieces.ml)[dst_row] = make_float2(m, l);
+                else if (p.lse)
+                    p.lse[dst_row] = lse_of(m, l);
+            }
+            next_piece();
+            if (!ok) break;
+            fetch_queries();
+            if (had.tiles > 0) {
+                ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.o_full[e]), n_o & 1u, kWaitSums, pieces));
+                if (!ok) break;
                 ++n_o;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            if (!ok) break;
-            if (threadIdx.x == (kPair ? 0 : e * 128)) w.note(p);
-            const bool at_once = w.is_whole() && p.n_groups == 0;
-            const float inv = at_once && l > 0.0f ? 1.0f / l : 0.0f;
-            float *dst = nullptr;
-            if (!at_once && real) {
-                float2 *ml;
-                if (w.is_whole()) {
-                    const Whole &to = p.whole[w.g.prefix ? 0 : 1];
-                    dst = to.o + row_at * D, ml = to.ml + row_at;
-                } else {
-                    const long long at = w.place() * kM + (kPair ? e * kWideRows : 0) + row;
-                    dst = p.pieces.o + at * D, ml = p.pieces.ml + at;
-                }
-                *ml = make_float2(m, l);
-            }
-            if (at_once && real && p.lse) p.lse[row_at] = lse_of(m, l);
-            char *out = p.out + (long long)(w.g.row0 + t) * p.out_stride + (long long)h * (D * 2);
+            if (had.rows == 0 || (had.tiles == 0 && !at_once)) continue; // (where l is 0 nobody reads the sums)
+            // Rows go out by way of the queries' place, 128 bytes of 32 rows at a time, so that a store fills whole lines (a thread that
+            // writes its own row keeps the load-store unit for 32 lines an instruction: a piece took 17000 cycles beside its tiles).
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            constexpr int kStep32 = 32, kStep16 = 64; // columns in 128 bytes
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
+            for (int c = 0; c < D; c += at_once ? kStep16 : kStep32) {
                 float o[32];
-                if (sr.tiles > 0) {
-                    tmem_ld32(o_at + c, o);
-                    tmem_wait_ld();
-                }
-                if (!real) continue;
-                if (at_once) {
+                uint32_t v[32];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = l > 0.0f ? pack2<T>(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv) : 0u;
-                        *reinterpret_cast<uint4 *>(out + (c + i) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                for (int k = 0; k < 2; ++k) {
+                    if (k == 1 && !at_once) break;
+                    if (had.tiles > 0) {
+                        tmem_ld32(o_at + c + k * 32, o);
+                        tmem_wait_ld();
                     }
-                } else if (sr.tiles > 0) { // (where l is 0 nobody reads them)
+                    if (at_once) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(dst + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        for (int i = 0; i < 16; ++i) v[k * 16 + i] = l > 0.0f ? pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv) : 0u;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(o[i]);
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                                 "r"(v[4 * i + 2]), "r"(v[4 * i + 3])
+                                 : "memory");
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = i * 4 + (lane >> 3), piece = lane & 7;
+                    const uint4 x = sweep::lds128(stage + r * 128 + ((piece ^ (r & 7)) << 4));
+                    const int d = __shfl_sync(0xffffffffu, dst_row, r), on = __shfl_sync(0xffffffffu, out_n, r), oh = __shfl_sync(0xffffffffu, out_h, r);
+                    if (d < 0) continue;
+                    if (at_once)
+                        *reinterpret_cast<uint4 *>(p.out + (long long)on * p.out_stride + (long long)oh * (D * 2) + c * 2 + piece * 16) = x;
+                    else
+                        *reinterpret_cast<uint4 *>(dst + (long long)d * D + c + piece * 4) = x;
+                }
+                __syncwarp();
             }
         }
     }
