@@ -32,8 +32,8 @@ using sweep::umma_desc;
 constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384, kWideCost = 2;
 constexpr int kPieces = 4;                      // that may wait for the softmax threads
 constexpr int kHalf = 16384;                    // bytes: 128 tokens (or rows) x 64 columns
-constexpr int kWideSmem = 14 * kHalf + 1024;    // queries and the rings; the base is aligned to 1 KB
-constexpr int kMaxPlaces = 12;
+constexpr int kWideSmem = 14 * kHalf + 1024;    // queries, the rings, 4 KB a softmax warp; the base is aligned to 1 KB
+constexpr int kMaxPlaces = 10;
 constexpr int kTmemCols = 512;
 // which wait gave up (status[1])
 enum { kWaitPlace = 110, kWaitKeys, kWaitValues, kWaitQueries, kWaitWeights, kWaitScores, kWaitSums, kWaitLastValues, kWaitPieces };
@@ -61,6 +61,13 @@ struct WideShared {
     PlanShared<2> plan;
 };
 
+// The queries of whole tokens and one KV head: 64 columns of all its query heads and of as many tokens as a tile holds.
+__device__ __forceinline__ void tma_queries(uint32_t dst, const CUtensorMap *tm, int x, int hk, int n, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(tm), "r"(x),
+                 "r"(0), "r"(hk), "r"(n), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t r;
@@ -131,12 +138,11 @@ struct Share {
     int rows, tiles;
 };
 __device__ __forceinline__ int sees(const PieceNote &g, int t) { return g.prefix ? g.len : clamp(g.len - g.n_q + t + 1, 0, g.len); }
-template <int kM>
-__device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, int e)
+__device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, int e, int rows)
 {
     Share s;
-    const int r0 = g.r0 + (kM > kWideRows ? e * kWideRows : 0);
-    s.rows = clamp(g.n_q * p.R - r0, 0, kWideRows);
+    const int r0 = g.r0 + e * rows;
+    s.rows = clamp(g.n_q * p.R - r0, 0, rows);
     const int vis = s.rows == 0 ? 0 : sees(g, (r0 + s.rows - 1) / p.R);
     s.tiles = max(0, min(g.b, (vis + kWideTile - 1) / kWideTile) - g.a);
     return s;
@@ -144,16 +150,18 @@ __device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, i
 
 template <typename T, int D, bool kPair>
 __global__ void __launch_bounds__(kWideThreads, 1)
-    attend_wide_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params p, int *status,
+    attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                       const Params p, int *status,
                        unsigned long long limit_cycles, int withhold)
 {
-    constexpr int kHalves = D / 64, kM = kPair ? 2 * kWideRows : kWideRows, kWorkers = kPair ? 1 : 2;
+    constexpr int kHalves = D / 64, kWorkers = kPair ? 1 : 2;
     constexpr int kPlace = kHalves * kHalf;                              // bytes: the keys, or the values, of a tile
-    constexpr int kPlaces = (14 - 2 * kHalves) / kHalves / kWorkers; // of a ring
+    constexpr int kPlaces = (12 - 2 * kHalves) / kHalves / kWorkers; // of a ring
     extern __shared__ unsigned char raw[];
     __shared__ WideShared sh;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rows = kPair ? p.pieces.M >> 1 : p.pieces.M; // of an engine: whole tokens, all of a KV head's query heads
     const auto q_at = [&](int e) { return base + (uint32_t)e * kPlace; };
     const auto place_at = [&](int ring, int i) { return base + (uint32_t)(2 + ring * kPlaces + i) * kPlace; };
 
@@ -174,7 +182,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             mbar_init(smem_u32(&sh.p_full[e]), 4);
             mbar_init(smem_u32(&sh.o_full[e]), 1);
             mbar_init(smem_u32(&sh.drain[e]), 1);
-            mbar_init(smem_u32(&sh.q_full[e]), 4);
+            mbar_init(smem_u32(&sh.q_full[e]), 1);
         }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -188,7 +196,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh.tmem;
     wait_for_previous();
-    plan<kM, kWideTile, kWideCost, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
+    plan<kWideTile, kWideCost, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
     const PlanShared<kWorkers> &pl = *reinterpret_cast<const PlanShared<kWorkers> *>(&sh.plan);
     const sweep::Ctl ctl{&sh.abort, status, limit_cycles};
 
@@ -199,13 +207,17 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
 
     if (warp >= 10) {
-        // ------------------------------------------------------------------ copies: one warp per ring, a lane per page
-        const int ring = warp - 10;
-        if (ring < kWorkers) {
-            Walk<kM, kWideTile, kWideCost> w;
+        // ------------------------------------------------------------------ copies: a lane per page
+        // Two rings: a warp each.  One ring: a warp for the keys and one for the values (pages of 16 tokens are 16 copies a place, and a
+        // warp takes 1300 cycles for them).
+        {
+            const int ring = kPair ? 0 : warp - 10, k0 = kPair ? warp - 10 : 0, k1 = kPair ? warp - 9 : 2;
+            const bool first = k0 == 0;
+            Walk<kWideTile, kWideCost> w;
             w.begin(p, pl, ring);
             const int box = min(1 << p.page_shift, kWideTile), nowhere = (p.n_pages * p.Hk) << p.page_shift;
-            uint32_t fills = 0, pieces = 0;
+            uint32_t tiles = 0, pieces = 0, last = 0; // of the ring so far; the warp's newest copy + 1
+            if (first && lane == 0) no_open_item(p, blockIdx.x * kWorkers + ring);
             bool ok = true;
             const auto announce = [&](const PieceNote &note) { // to the softmax threads
                 const int at = (int)(pieces % kPieces);
@@ -220,9 +232,14 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 ++pieces;
             };
             for (; ok && !w.done; w.next(p)) {
-                const PieceNote piece{w.g.row0, w.g.n_q, w.g.len, w.hk, w.mb * kM, w.a, w.b, w.vis, w.is_whole() ? kToRows : (int)w.place(), (int)w.g.prefix};
-                if (lane == 0) w.note(p);
-                announce(piece);
+                const PieceNote piece{w.g.row0, w.g.n_q, w.g.len, w.hk, w.mb * p.pieces.M, w.a, w.b, w.vis, w.is_whole() ? kToRows : (int)w.place(), (int)w.g.prefix};
+                if (first) {
+                    if (lane == 0) {
+                        w.note(p);
+                        if (w.a == 0 && w.b < w.nt) open_item(p, w);
+                    }
+                    announce(piece);
+                }
                 if (!ok) break;
                 const auto page_row = [&](int tile) { // where the lane's page of a tile begins among all rows of the cache
                     const int tok = tile * kWideTile + lane * box;
@@ -234,7 +251,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                     return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
                 };
-                const Share s0 = share_of<kM>(p, piece, 0), s1 = kPair ? share_of<kM>(p, piece, 1) : Share{0, 0};
+                const Share s0 = share_of(p, piece, 0, rows), s1 = kPair ? share_of(p, piece, 1, rows) : Share{0, 0};
                 int next_row = page_row(w.a);
                 for (int tile = w.a; ok && tile < w.b; ++tile) {
                     const int row = next_row;
@@ -243,11 +260,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     const uint32_t note = (i_tile < s0.tiles ? 1u : 0u) | (i_tile < s1.tiles ? 2u : 0u) | (i_tile == 0 ? kNoteFirst : 0u) |
                                           (i_tile == s0.tiles - 1 ? kNoteLast : 0u) | (i_tile == s1.tiles - 1 ? 2 * kNoteLast : 0u) | (uint32_t)((tokens + 15) >> 4) << 8;
 #pragma unroll 1
-                    for (int i = 0; ok && i < 2; ++i) {
-                        const int at = (int)(fills % kPlaces);
+                    for (int i = k0; ok && i < k1; ++i) {
+                        const uint32_t fill = 2 * tiles + i;
+                        const int at = (int)(fill % kPlaces);
                         const uint32_t bar = smem_u32(&sh.full[ring][at]);
                         if (lane == 0) {
-                            ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, w.item());
+                            ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fill / kPlaces) & 1u) ^ 1u, kWaitPlace, fill);
                             if (ok) {
                                 sh.note[ring][at] = note;
                                 mbar_arrive_expect_tx(bar, (uint32_t)(n * box * 128 * kHalves));
@@ -255,27 +273,27 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         }
                         ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
                         if (!ok) break;
-                        ++fills;
+                        last = fill + 1;
                         if (lane < n)
 #pragma unroll
                             for (int h = 0; h < kHalves; ++h) tma_page(place_at(ring, at) + h * kHalf + lane * box * 128, i ? &tm_v : &tm_k, h * 64, row, bar);
                     }
+                    ++tiles;
                 }
             }
-            if (ok) announce(PieceNote{0, 0, 0, 0, 0, 0, -1, 0, 0, 0});
-            if (ok && lane == 0) { // nothing follows
-                const int at = (int)(fills % kPlaces);
-                ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fills / kPlaces) & 1u) ^ 1u, kWaitPlace, -1);
+            if (first && ok) announce(PieceNote{0, 0, 0, 0, 0, 0, -1, 0, 0, 0});
+            if (first && ok && lane == 0) { // nothing follows
+                const uint32_t fill = 2 * tiles;
+                const int at = (int)(fill % kPlaces);
+                ok = ctl.wait_bar(smem_u32(&sh.empty[ring][at]), ((fill / kPlaces) & 1u) ^ 1u, kWaitPlace, fill);
                 if (ok) {
                     sh.note[ring][at] = kNoteEnd;
                     mbar_arrive(smem_u32(&sh.full[ring][at]));
                 }
             }
             if (!ok && lane == 0) // a CTA does not end before its copies have landed
-                for (uint32_t i = 0; i < (uint32_t)kPlaces; ++i) {
-                    const uint32_t n = fills > i ? (fills - i - 1) / kPlaces + 1 : 0;
-                    if (n) ctl.wait_landed(smem_u32(&sh.full[ring][i]), (n - 1) & 1u);
-                }
+                for (uint32_t f = last > (uint32_t)kPlaces ? last - kPlaces : 0; f < last; ++f)
+                    if (!kPair || (int)(f & 1u) == k0) ctl.wait_landed(smem_u32(&sh.full[ring][f % kPlaces]), (f / kPlaces) & 1u);
             __syncwarp();
         }
     } else if (warp >= 8) {
@@ -356,32 +374,36 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 }
             }
             while (ok && !(note & kNoteEnd)) {
-                // a tile's values, and the next one's keys: per engine the sums of the one, then the scores of the other, so that
-                // one engine's softmax runs beside the other one's products
+                // a tile's values, and the next one's keys if they are there: per engine the sums of the one, then the scores of the
+                // other, so that one engine's softmax runs beside the other one's products
                 ok = wait(full + at * 8, round, kWaitValues);
                 if (!ok) break;
                 const int at_v = next_place();
-                ok = wait(full + at * 8, round, kWaitKeys);
-                if (!ok) break;
-                const uint32_t next = sh.note[ring][at];
-                const bool fresh = (next & (kNoteFirst | kNoteEnd)) != 0; // a piece ends: the engines' sums are not held up by each other's end
+                const bool ready = __all_sync(0xffffffffu, sweep::mbar_try_wait(full + at * 8, round)) != 0;
+                uint32_t next = ready ? sh.note[ring][at] : kNoteFirst;
+                const bool along = !(next & (kNoteFirst | kNoteEnd)); // (where a piece ends the engines do not wait for each other's end)
                 if (kPair) {
                     if (note & 1u) ok = sums(0, at_v, note);
-                    if (ok && !fresh && (next & 1u)) scores(0, at);
+                    if (ok && along && (next & 1u)) scores(0, at);
                     if (ok && (note & 2u)) ok = sums(1, at_v, note);
-                    if (ok && !fresh && (next & 2u)) scores(1, at);
+                    if (ok && along && (next & 2u)) scores(1, at);
                 } else if (note & 1u) {
                     ok = sums(ring, at_v, note);
-                    if (ok && !fresh && (next & 1u)) scores(ring, at);
+                    if (ok && along && (next & 1u)) scores(ring, at);
                 }
                 if (!ok) break;
                 release(at_v);
+                if (!ready) {
+                    ok = wait(full + at * 8, round, kWaitKeys);
+                    if (!ok) break;
+                    next = sh.note[ring][at];
+                }
                 note = next;
                 if (note & kNoteEnd) break;
-                if (fresh)
+                if (!along)
                     for (int e = 0; ok && e < (kPair ? 2 : 1); ++e)
                         if (note >> e & 1u) {
-                            ok = queries(ring + e);
+                            if (note & kNoteFirst) ok = queries(ring + e);
                             if (ok) scores(ring + e, at);
                         }
                 if (!ok) break;
@@ -397,60 +419,38 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // ------------------------------------------------------------------ softmax: a thread per row
         const int e = warp >> 2, ring = kPair ? 0 : e, row = (warp & 3) * 32 + lane;
         const uint32_t s_at = tmem + e * 256 + ((uint32_t)((warp & 3) * 32) << 16), o_at = s_at + 128;
-        const uint32_t stage = q_at(e) + (warp & 3) * 32 * 128; // the warp's rows of the queries (first half of their columns)
+        const uint32_t stage = base + (uint32_t)(2 + kWorkers * kPlaces) * kPlace + warp * 4096;
+        const int off = kPair ? e * rows : 0;                        // of the engine's first row
         uint32_t seen = 0, n_s = 0, n_o = 0, pieces = 0; // tiles of the ring passed so far; phases
         bool ok = true;
-        PieceNote w{0, 0, 0, 0, 0, 0, -1, 0, 0, 0};
+        const PieceNote *w = &sh.piece[ring][0]; // (read where it is wanted: registers are for scores)
         Share sr{0, 0};
-        int n = 0, h = 0, lim = 0; // the thread's row: packed row and head; how many tokens it sees
-        bool real = false;
+        int n0 = 0, lim = 0, begin = 0, end = -1; // the engine's first packed row; how many tokens the thread's row sees; the piece's tiles
+        // The next piece, and its queries: the scores of the piece before are all there, so that nobody reads its queries any more.
         const auto next_piece = [&]() {
             const int at = (int)(pieces % kPieces);
             ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.piece_full[ring][at]), (pieces / kPieces) & 1u, kWaitPieces, pieces));
             if (!ok) return;
-            w = sh.piece[ring][at];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.piece_empty[ring][at]));
+            w = &sh.piece[ring][at];
             ++pieces;
-            if (w.b < 0) return;
-            sr = share_of<kM>(p, w, e);
-            const int r = w.r0 + (kPair ? e * kWideRows : 0) + row;
-            real = row < sr.rows;
-            const int t = real ? r / p.R : 0;
-            n = w.row0 + t, h = w.hk * p.R + (real ? r - t * p.R : 0);
-            lim = real ? sees(w, t) : w.vis;
-        };
-        // Queries: 16 (8) lanes a row, so that a load takes whole lines.
-        constexpr int kRowLanes = D / 8, kRowsPer = 32 / kRowLanes;
-        uint4 q[kRowLanes];
-        const auto fetch_queries = [&]() { // (always all of q: nothing of the piece before stays in registers)
-            const bool any = w.b >= 0 && sr.tiles > 0;
+            begin = w->a, end = w->b;
+            if (end < 0) return;
+            sr = share_of(p, *w, kPair ? e : 0, rows);
+            const int t0 = (w->r0 + off) / p.R;
+            n0 = w->row0 + t0;
+            lim = row < sr.rows ? sees(*w, t0 + row / p.R) : w->vis;
+            if (sr.tiles > 0 && (warp & 3) == 0 && lane == 0) {
+                // rows behind the segment's last are whatever comes next: nobody reads what comes of them
+                const uint32_t bar = smem_u32(&sh.q_full[e]);
+                mbar_arrive_expect_tx(bar, (uint32_t)(rows * D * 2));
 #pragma unroll
-            for (int i = 0; i < kRowLanes; ++i) {
-                const int from = i * kRowsPer + lane / kRowLanes;
-                const int qn = __shfl_sync(0xffffffffu, n, from), qh = __shfl_sync(0xffffffffu, h, from);
-                const bool there = __shfl_sync(0xffffffffu, (int)real, from) != 0;
-                q[i] = any && there ? *reinterpret_cast<const uint4 *>(p.q + (long long)qn * p.q_stride + (long long)qh * (D * 2) + (lane % kRowLanes) * 16) : make_uint4(0, 0, 0, 0);
+                for (int hh = 0; hh < kHalves; ++hh) tma_queries(q_at(e) + hh * kHalf, &tm_q, hh * 64, w->hk, n0, bar);
             }
         };
         next_piece();
-        fetch_queries();
-        while (ok && w.b >= 0) {
+        while (ok && end >= 0) {
             float m = -INFINITY, l = 0.0f;
-            if (sr.tiles > 0) {
-                // swizzled as a TMA copy would leave them (the piece before has ended with all its products)
-#pragma unroll
-                for (int i = 0; i < kRowLanes; ++i) {
-                    const int c = lane % kRowLanes, r = (warp & 3) * 32 + i * kRowsPer + lane / kRowLanes;
-                    const uint32_t dst = q_at(e) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(q[i].x), "r"(q[i].y), "r"(q[i].z), "r"(q[i].w) : "memory");
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[e]));
-            }
-            for (int tile = w.a; ok && tile < w.a + sr.tiles; ++tile) {
+            for (int tile = begin; ok && tile < begin + sr.tiles; ++tile) {
                 ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.s_full[e]), n_s & 1u, kWaitScores, pieces));
                 if (!ok) break;
                 ++n_s;
@@ -463,9 +463,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 if (__any_sync(0xffffffffu, n_see < kWideTile))
 #pragma unroll
                     for (int i = 0; i < 128; ++i) s[i] = i < n_see ? s[i] : -INFINITY;
-                const int n_here = w.vis - tile * kWideTile; // tokens behind the last one: their values must be zeros up to the product's end
+                const int n_here = w->vis - tile * kWideTile; // tokens behind the last one: their values must be zeros up to the product's end
                 if (n_here < kWideTile && (n_here & 15)) {
-                    const uint32_t fill = (seen + (tile - w.a)) * 2 + 1;
+                    const uint32_t fill = (seen + (tile - begin)) * 2 + 1;
                     const int at = (int)(fill % kPlaces), n_zero = 16 - (n_here & 15);
                     ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.full[ring][at]), (fill / kPlaces) & 1u, kWaitLastValues, pieces));
 #pragma unroll
@@ -479,9 +479,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
                 for (int i = 4; i < 128; i += 4) t0 = fmaxf(t0, s[i]), t1 = fmaxf(t1, s[i + 1]), t2 = fmaxf(t2, s[i + 2]), t3 = fmaxf(t3, s[i + 3]);
                 const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * p.scale_log2;
-                if (__any_sync(0xffffffffu, top > m + 8.0f)) { // (from -inf: any)
+                if (__any_sync(0xffffffffu, row < sr.rows && top > m + 8.0f)) { // (from -inf: any; rows of nobody hold whatever was there)
                     const float now = fmaxf(m, top), fix = m == now ? 1.0f : exp2_approx(m - now);
-                    if (tile > w.a) { // (this tile's scores being there, the products before them have ended)
+                    if (tile > begin) { // (this tile's scores being there, the products before them have ended)
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
                             uint32_t o[16];
@@ -519,53 +519,44 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 l += (l0 + l1) + (l2 + l3);
             }
             if (!ok) break;
-            seen += w.b - w.a;
+            seen += end - begin;
             // what the piece leaves, and where; then, while its last products run, the next one's queries are asked for
             const Share had = sr;
-            const bool at_once = w.place == kToRows && p.n_groups == 0, was_real = real;
-            const Whole &to = p.whole[w.prefix ? 0 : 1];
-            const int out_n = n, out_h = h;
-            const int dst_row = !real ? -1 : w.place == kToRows ? n * p.Hq + h : w.place * kM + (kPair ? e * kWideRows : 0) + row;
-            float *const dst = w.place == kToRows ? to.o : p.pieces.o;
-            if (was_real) {
-                if (!at_once)
-                    (w.place == kToRows ? to.ml : p.pieces.ml)[dst_row] = make_float2(m, l);
-                else if (p.lse)
-                    p.lse[dst_row] = lse_of(m, l);
+            const uint32_t inv_R = (65536u + p.R - 1) / (uint32_t)p.R; // row / R for rows below 128: (row * inv_R) >> 16
+            const int my_t = (int)(row * inv_R >> 16), my_h = row - my_t * p.R;
+            const bool by_row = w->place == kToRows, at_once = by_row && p.n_groups == 0;
+            const int h0 = w->hk * p.R;
+            char *dst;             // of the engine's first row; the next token's and the next head's are so far on
+            long long per_t, per_h;
+            if (at_once) {
+                per_t = p.out_stride, per_h = D * 2;
+                dst = p.out + (long long)n0 * p.out_stride + (long long)h0 * (D * 2);
+            } else {
+                per_t = (long long)(by_row ? p.Hq : p.R) * (D * 4), per_h = D * 4;
+                dst = (char *)(by_row ? p.whole[w->prefix ? 0 : 1].o : p.pieces.o) + (by_row ? (long long)n0 * p.Hq + h0 : (long long)w->place * p.pieces.M + off) * (D * 4);
             }
+            if (row < had.rows) {
+                const long long at = by_row ? (long long)(n0 + my_t) * p.Hq + h0 + my_h : (long long)w->place * p.pieces.M + off + row;
+                if (!at_once)
+                    (by_row ? p.whole[w->prefix ? 0 : 1].ml : p.pieces.ml)[at] = make_float2(m, l);
+                else if (p.lse)
+                    p.lse[at] = lse_of(m, l);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.piece_empty[ring][(pieces - 1) % kPieces]));
             next_piece();
             if (!ok) break;
-            fetch_queries();
             if (had.tiles > 0) {
                 ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.o_full[e]), n_o & 1u, kWaitSums, pieces));
                 if (!ok) break;
                 ++n_o;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            if (had.rows == 0 || (had.tiles == 0 && !at_once)) continue; // (where l is 0 nobody reads the sums)
-            // Rows go out by way of the queries' place, 128 bytes of 32 rows at a time, so that a store fills whole lines (a thread that
+            if (had.tiles == 0 && !at_once) continue; // (where l is 0 nobody reads the sums)
+            // Rows go out by way of shared memory, 128 bytes of 32 rows at a time, so that a store fills whole lines (a thread that
             // writes its own row keeps the load-store unit for 32 lines an instruction: a piece took 17000 cycles beside its tiles).
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            constexpr int kStep32 = 32, kStep16 = 64; // columns in 128 bytes
-#pragma unroll 1
-            for (int c = 0; c < D; c += at_once ? kStep16 : kStep32) {
-                float o[32];
-                uint32_t v[32];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (k == 1 && !at_once) break;
-                    if (had.tiles > 0) {
-                        tmem_ld32(o_at + c + k * 32, o);
-                        tmem_wait_ld();
-                    }
-                    if (at_once) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[k * 16 + i] = l > 0.0f ? pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv) : 0u;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(o[i]);
-                    }
-                }
+            const auto out_128 = [&](const uint32_t *v, int c) { // the thread's 128 bytes, c bytes into the rows
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(v[4 * i]), "r"(v[4 * i + 1]),
@@ -574,16 +565,34 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int r = i * 4 + (lane >> 3), piece = lane & 7;
-                    const uint4 x = sweep::lds128(stage + r * 128 + ((piece ^ (r & 7)) << 4));
-                    const int d = __shfl_sync(0xffffffffu, dst_row, r), on = __shfl_sync(0xffffffffu, out_n, r), oh = __shfl_sync(0xffffffffu, out_h, r);
-                    if (d < 0) continue;
-                    if (at_once)
-                        *reinterpret_cast<uint4 *>(p.out + (long long)on * p.out_stride + (long long)oh * (D * 2) + c * 2 + piece * 16) = x;
-                    else
-                        *reinterpret_cast<uint4 *>(dst + (long long)d * D + c + piece * 4) = x;
+                    const int in_warp = i * 4 + (lane >> 3), r = (warp & 3) * 32 + in_warp, piece = lane & 7;
+                    const int t = (int)(r * inv_R >> 16), hh = r - t * p.R;
+                    const uint4 x = sweep::lds128(stage + in_warp * 128 + ((piece ^ (in_warp & 7)) << 4));
+                    if (r < had.rows) *reinterpret_cast<uint4 *>(dst + t * per_t + hh * per_h + c + piece * 16) = x;
                 }
                 __syncwarp();
+            };
+            if (at_once) {
+#pragma unroll 1
+                for (int c = 0; c < D; c += 64) {
+                    float o[64];
+                    uint32_t v[32];
+                    if (had.tiles > 0) {
+                        tmem_ld32(o_at + c, o), tmem_ld32(o_at + c + 32, o + 32);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = l > 0.0f ? pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv) : 0u;
+                    out_128(v, c * 2);
+                }
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    float o[32];
+                    tmem_ld32(o_at + c, o);
+                    tmem_wait_ld();
+                    out_128(reinterpret_cast<const uint32_t *>(o), c * 4);
+                }
             }
         }
     }

@@ -93,7 +93,8 @@ size_t cache_bytes(const dart_cache *c) { return (size_t)c->n_pages * c->n_heads
 
 // ---- attention ---------------------------------------------------------------------------------------------------------------
 
-constexpr int kJoinWide = 4096; // (row, head) pairs up to which four warps join one
+constexpr int kJoinFew = 2048;   // (row, head) pairs up to which eight warps join one
+constexpr int kJoinMany = 16384; // ... and one warp; beyond, a warp joins eight
 
 enum Form { NARROW, WIDE, PAIR };
 
@@ -101,7 +102,7 @@ struct Launch {
     bool prefix, own;
     Form form;
     int M, n_workers, max_items, n_seg;
-    size_t item_base, items, ml, o; // places in the workspace
+    size_t item_base, items, open, ml, o; // places in the workspace
 };
 struct Layout {
     Launch launch[2];
@@ -110,10 +111,11 @@ struct Layout {
 };
 
 // Rows of a tile by how many rows a segment has on average (the host knows the sizes, not the lengths).
-Form form_of(long long rows, long long segments)
+// A wide tile holds whole tokens, so that a copy can fetch its queries.
+Form form_of(long long rows, long long segments, long long R)
 {
-    const long long avg = (rows + segments - 1) / segments;
-    return avg <= dart::attend::kNarrowM ? NARROW : avg <= dart::attend::kWideRows ? WIDE : PAIR;
+    const long long avg = (rows + segments - 1) / segments, wide = dart::attend::kWideRows / R * R;
+    return avg <= dart::attend::kNarrowM || wide == 0 ? NARROW : avg <= wide ? WIDE : PAIR;
 }
 
 int sm_count_of(int device)
@@ -132,7 +134,7 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     using namespace dart::attend;
     Layout L = {};
     const long long R = a->n_q_heads / c->n_heads;
-    const Form own = form_of(a->n_rows * R, a->n_seq), shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups) : own;
+    const Form own = form_of(a->n_rows * R, a->n_seq, R), shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups, R) : own;
     L.n = own == shared ? 1 : 2;
     L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = own == shared, L.launch[0].form = shared;
     L.launch[1].own = true, L.launch[1].form = own;
@@ -144,7 +146,8 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     };
     for (int i = 0; i < L.n; ++i) {
         Launch &l = L.launch[i];
-        l.M = l.form == NARROW ? kNarrowM : l.form == WIDE ? kWideRows : 2 * kWideRows;
+        const int wide = (int)(kWideRows / R * R);
+        l.M = l.form == NARROW ? kNarrowM : l.form == WIDE ? wide : 2 * wide;
         l.n_workers = sms * (l.form == NARROW ? kNarrowWarps : l.form == WIDE ? 2 : 1);
         l.n_seg = (l.prefix ? a->n_groups : 0) + (l.own ? a->n_seq : 0);
         const long long more = a->n_rows * R / l.M; // a segment of n rows has at most 1 + n / M tiles
@@ -152,6 +155,7 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
         l.max_items = items < 2147483647ll ? (int)items : 2147483647;
         l.item_base = take(sizeof(int) * ((size_t)l.n_seg + 1));
         l.items = take(sizeof(int2) * (size_t)l.max_items);
+        l.open = take(sizeof(Open) * l.n_workers);
         l.ml = take(sizeof(float2) * 2 * l.n_workers * l.M);
         l.o = take(sizeof(float) * 2 * l.n_workers * (size_t)l.M * c->head_dim);
     }
@@ -220,6 +224,19 @@ bool encode_cache(CUtensorMap *tm, const dart_cache *c, void *base)
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The queries as [rows][KV heads][query heads of each][columns]; a box is the tokens of a tile, one KV head, 64 columns, swizzled.
+bool encode_queries(CUtensorMap *tm, const dart_cache *c, const dart_attend_args *a)
+{
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t R = (cuuint64_t)(a->n_q_heads / c->n_heads), D = (cuuint64_t)c->head_dim;
+    const cuuint64_t row = a->n_rows > 1 ? (cuuint64_t)a->q_stride : R * D * c->n_heads;
+    const cuuint64_t dims[4] = {D, R, (cuuint64_t)c->n_heads, (cuuint64_t)a->n_rows}, strides[3] = {D * 2, R * D * 2, row * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)R, 1, (cuuint32_t)(dart::attend::kWideRows / R)}, one[4] = {1, 1, 1, 1};
+    return fn(tm, c->dtype == DART_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(a->q), dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename K>
 cudaError_t with_smem(K kernel, size_t smem)
 {
@@ -241,13 +258,13 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     p.scale_log2 = a->scale * 1.44269504088896340736f, p.status = a->status;
     for (int k = 0; k < 2; ++k) p.whole[k] = Whole{(float *)(ws + L.whole_o[k]), (float2 *)(ws + L.whole_ml[k])};
     JoinParams j = {};
-    CUtensorMap tm_k, tm_v;
+    CUtensorMap tm_q, tm_k, tm_v;
     bool maps = false;
     for (int i = 0; i < L.n; ++i) {
         const Launch &l = L.launch[i];
         p.n_prefix = l.prefix ? a->n_groups : 0, p.n_own = l.own ? a->n_seq : 0;
         p.n_workers = l.n_workers, p.min_tiles = 1, p.max_items = l.max_items;
-        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), l.M, l.n_workers};
+        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), (Open *)(ws + l.open), l.M, l.n_workers};
         for (int k = 0; k < 2; ++k)
             if (k ? l.own : l.prefix) j.from[k] = p.pieces, j.seg_off[k] = k ? p.n_prefix : 0, j.n_seg[k] = l.n_seg;
         cudaError_t e;
@@ -256,13 +273,13 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
             e = with_smem(attend_narrow_kernel<T, D>, smem);
             if (e == cudaSuccess) e = launch_next(attend_narrow_kernel<T, D>, dim3(sms), kNarrowWarps * 32, smem, st, p);
         } else {
-            if (!maps && (!encode_cache(&tm_k, c, c->k) || !encode_cache(&tm_v, c, c->v))) return DART_ERR_CUDA;
+            if (!maps && (!encode_queries(&tm_q, c, a) || !encode_cache(&tm_k, c, c->k) || !encode_cache(&tm_v, c, c->v))) return DART_ERR_CUDA;
             maps = true;
             const auto kernel = l.form == PAIR ? attend_wide_kernel<T, D, true> : attend_wide_kernel<T, D, false>;
             const unsigned long long limit = (a->wait_limit > 0 ? (unsigned long long)a->wait_limit : 2000000ull) * 2100ull;
             e = with_smem(kernel, kWideSmem);
             if (e == cudaSuccess)
-                e = launch_next(kernel, dim3(sms), kWideThreads, kWideSmem, st, tm_k, tm_v, p, a->status ? (int *)a->status : (int *)(ws + L.status), limit,
+                e = launch_next(kernel, dim3(sms), kWideThreads, kWideSmem, st, tm_q, tm_k, tm_v, p, a->status ? (int *)a->status : (int *)(ws + L.status), limit,
                                 a->test_withhold);
         }
         if (e != cudaSuccess) {
@@ -272,8 +289,11 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     }
     j.p = p;
     const long long pairs = (long long)a->n_rows * a->n_q_heads;
-    const cudaError_t e = pairs <= kJoinWide ? launch_next(attend_join_kernel<T, D, 4>, dim3((unsigned)pairs), 128, 0, st, j)
-                                             : launch_next(attend_join_kernel<T, D, 1>, dim3((unsigned)((pairs + 3) / 4)), 128, 0, st, j);
+    const int heads = pairs <= kJoinMany ? 1 : 8;
+    const long long warps = a->n_rows * ((a->n_q_heads + heads - 1ll) / heads);
+    const cudaError_t e = pairs <= kJoinFew       ? launch_next(attend_join_rows_kernel<T, D, 8>, dim3((unsigned)pairs), 256, 0, st, j, 1)
+                          : a->n_groups > 0 ? launch_next(attend_join_rows_kernel<T, D, 1>, dim3((unsigned)((warps + 3) / 4)), 128, 0, st, j, heads)
+                                            : launch_next(attend_join_cut_kernel<T, D>, dim3((unsigned)j.from[1].n_workers), 256, 0, st, p, j.from[1]);
     const cudaError_t e2 = cudaGetLastError();
     return e == cudaSuccess && e2 == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
