@@ -371,8 +371,6 @@ int dart_pivots_static(const void *keys, int B, int S, int d, int vis_offset, in
  * Angles are taken in fp64, so that far and negative positions lose nothing. */
 typedef struct {
     const float *inv_freq; /* [rot_dim / 2] device */
-    const int64_t *pos;    /* device: [n_axes][pos_stride], row n's position(s) at n, n + pos_stride, ... */
-    int64_t pos_stride;    /* values from axis to axis (>= n_rows; any with one axis) */
     int32_t rot_dim;       /* a multiple of 16, at most head_dim; 0: no rotation */
     int32_t interleaved;
     int32_t n_axes;        /* 0 or 1: one position a row; 2, 3: time, height, width of vision tokens: the first section[0] pairs turn
@@ -386,7 +384,8 @@ typedef struct {
  *   q, k           [n_rows] rows of n_q_heads / n_k_heads heads, device, 16-byte aligned; either may have 0 heads (then its
  *                  pointers are not looked at)
  *   q_weight, k_weight [head_dim] of the rows' type, device, 16-byte aligned, or NULL: no norm
- *   rope           NULL or rot_dim 0: no rotation
+ *   rope           NULL or rot_dim 0: no rotation (pos is then not looked at)
+ *   pos            int64 device: [n_axes][pos_stride], row n's position(s) at n, n + pos_stride, ...; pos_stride >= n_rows (any with one axis)
  *   q_out, k_out   rows as q and k; may be q and k themselves (same pointer and stride) or columns of one buffer, else they must
  *                  not share a byte with any input or with each other
  * Limits: head_dim a multiple of 8 up to 256; at most 65536 heads in all; n_rows 0 does nothing.
@@ -394,7 +393,7 @@ typedef struct {
  */
 int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k, int64_t k_stride, int n_k_heads, int n_rows,
                    int head_dim, int dtype, const void *q_weight, const void *k_weight, float eps, const dart_rope *rope,
-                   void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream);
+                   const int64_t *pos, int64_t pos_stride, void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream);
 
 /* A paged cache of keys and values: each [n_pages][n_heads][page_size][head_dim], dense, 16-byte aligned, on `device`.  A sequence's
  * token number s lies in page table[sequence][s / page_size] at place s % page_size. */
@@ -414,7 +413,7 @@ typedef struct {
  *   idx         NULL: packed row n is row n of k and v; else [n_rows] int32 device: it is row b * S + idx[n]
  *   table       [n_seq][table_stride] int32 device; only the entries of written slots are read.  No two rows may have the same slot
  *   start       [n_seq] int32 device: tokens that the cache already holds, or NULL: none
- *   k_weight, eps, rope  as in dart_norm_rope, for the keys; rope->pos is by packed row; NULL: the slot is the position
+ *   k_weight, eps, rope, pos  as in dart_norm_rope, for the keys; pos is by packed row; NULL: the slot is the position (one axis only)
  *   status      [4] int32 device, or NULL.  A row whose slot is outside its table row, whose page is outside the cache or whose idx is
  *               outside [0, S) is left out, and status[0] becomes DART_ERR_CHECK
  * cache->page_size may be any positive number here.  n_rows 0 does nothing.
@@ -422,7 +421,8 @@ typedef struct {
  */
 int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int n_seq,
                       int n_rows, const int32_t *cu_rows, const int32_t *idx, int S, const int32_t *table, int table_stride,
-                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, int32_t *status, void *stream);
+                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, const int64_t *pos,
+                      int64_t pos_stride, int32_t *status, void *stream);
 
 /*
  * Attention over a paged cache.  Sequence b has the query rows cu_q[b] .. cu_q[b + 1] - 1 (n of them) and kv_len[b] tokens in its

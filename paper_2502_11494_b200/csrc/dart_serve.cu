@@ -4,6 +4,8 @@
 
 #include <math.h>
 
+#include <atomic>
+
 #include <cuda.h>
 
 #include "dart_attend.cuh"
@@ -24,13 +26,13 @@ bool rows_overlap(const void *a, long long na, long long sa, long long wa, const
     return d < wa || sa - d < wb;
 }
 
-int check_rope(const dart_rope *r, int head_dim, int n_rows, bool need_pos)
+int check_rope(const dart_rope *r, const int64_t *pos, int64_t pos_stride, int head_dim, int n_rows, bool need_pos)
 {
     if (!r || r->rot_dim == 0) return DART_OK;
-    if (!r->inv_freq || (need_pos && !r->pos)) return DART_ERR_NULL;
+    if (!r->inv_freq || (need_pos && !pos)) return DART_ERR_NULL;
     if (r->rot_dim < 0 || r->rot_dim % 16 != 0 || r->rot_dim > head_dim || r->n_axes < 0 || r->n_axes > 3) return DART_ERR_BAD_SHAPE;
     if (r->n_axes > 1) {
-        if (r->pos && r->pos_stride < n_rows) return DART_ERR_BAD_SHAPE;
+        if (pos && pos_stride < n_rows) return DART_ERR_BAD_SHAPE;
         long long sum = 0;
         for (int a = 0; a < r->n_axes; ++a) {
             if (r->section[a] < 0) return DART_ERR_BAD_SHAPE;
@@ -38,11 +40,11 @@ int check_rope(const dart_rope *r, int head_dim, int n_rows, bool need_pos)
         }
         if (sum != r->rot_dim / 2) return DART_ERR_BAD_SHAPE;
     }
-    if (misaligned(r->inv_freq, 4) || misaligned(r->pos, 8)) return DART_ERR_ALIGN;
+    if (misaligned(r->inv_freq, 4) || misaligned(pos, 8)) return DART_ERR_ALIGN;
     return DART_OK;
 }
 
-void set_rope(dart::rows::Params &p, const dart_rope *r)
+void set_rope(dart::rows::Params &p, const dart_rope *r, const int64_t *pos, int64_t pos_stride)
 {
     p.half = 0;
     if (!r || r->rot_dim == 0) return;
@@ -50,7 +52,7 @@ void set_rope(dart::rows::Params &p, const dart_rope *r)
     p.n_axes = r->n_axes > 1 ? r->n_axes : 1;
     p.sec0 = r->n_axes > 1 ? r->section[0] : p.half;
     p.sec01 = r->n_axes > 2 ? r->section[0] + r->section[1] : p.half; // (two axes: no pair turns by a third)
-    p.inv_freq = r->inv_freq, p.pos = r->pos, p.pos_stride = r->pos_stride;
+    p.inv_freq = r->inv_freq, p.pos = pos, p.pos_stride = pos_stride;
 }
 
 bool known_type(int dtype) { return dtype == DART_BF16 || dtype == DART_FP16; }
@@ -120,11 +122,14 @@ Form form_of(long long rows, long long segments, long long R)
 
 int sm_count_of(int device)
 {
+    static std::atomic<int> known[64]; // zero: not asked yet
+    if (device >= 0 && device < 64 && known[device].load(std::memory_order_relaxed)) return known[device].load(std::memory_order_relaxed);
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) {
         cudaGetLastError();
-        n = 148;
+        return 148;
     }
+    if (device >= 0 && device < 64) known[device].store(n, std::memory_order_relaxed);
     return n;
 }
 
@@ -304,7 +309,7 @@ extern "C" {
 
 int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k, int64_t k_stride, int n_k_heads, int n_rows,
                    int head_dim, int dtype, const void *q_weight, const void *k_weight, float eps, const dart_rope *rope,
-                   void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream)
+                   const int64_t *pos, int64_t pos_stride, void *q_out, int64_t qo_stride, void *k_out, int64_t ko_stride, int device, void *stream)
 {
     if (n_rows < 0 || n_q_heads < 0 || n_k_heads < 0 || n_q_heads + (long long)n_k_heads < 1 || n_q_heads + (long long)n_k_heads > 65536 ||
         head_dim < 8 || head_dim > 256 || head_dim % 8 != 0 || !(eps >= 0.0f) || isinf(eps))
@@ -315,7 +320,7 @@ int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k
     if (!head_rows_ok(n_q_heads, head_dim, q_stride, n_rows) || !head_rows_ok(n_q_heads, head_dim, qo_stride, n_rows) ||
         !head_rows_ok(n_k_heads, head_dim, k_stride, n_rows) || !head_rows_ok(n_k_heads, head_dim, ko_stride, n_rows))
         return DART_ERR_BAD_SHAPE;
-    int rc = check_rope(rope, head_dim, n_rows, true);
+    int rc = check_rope(rope, pos, pos_stride, head_dim, n_rows, true);
     if (rc != DART_OK) return rc;
     if (!n_q_heads) q = q_out = nullptr, q_weight = nullptr;
     if (!n_k_heads) k = k_out = nullptr, k_weight = nullptr;
@@ -335,13 +340,14 @@ int dart_norm_rope(const void *q, int64_t q_stride, int n_q_heads, const void *k
     p.side[0] = {(const char *)q, (char *)q_out, (const char *)q_weight, 2 * q_stride, 2 * qo_stride, n_q_heads, true};
     p.side[1] = {(const char *)k, (char *)k_out, (const char *)k_weight, 2 * k_stride, 2 * ko_stride, n_k_heads, true};
     p.n_rows = n_rows, p.D = head_dim, p.eps = eps;
-    set_rope(p, rope);
+    set_rope(p, rope, pos, pos_stride);
     return dtype == DART_BF16 ? launch_rows<__nv_bfloat16, false>(p, (cudaStream_t)stream) : launch_rows<__half, false>(p, (cudaStream_t)stream);
 }
 
 int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int n_seq,
                       int n_rows, const int32_t *cu_rows, const int32_t *idx, int S, const int32_t *table, int table_stride,
-                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, int32_t *status, void *stream)
+                      const int32_t *start, const void *k_weight, float eps, const dart_rope *rope, const int64_t *pos, int64_t pos_stride,
+                      int32_t *status, void *stream)
 {
     int rc = check_cache(cache);
     if (rc != DART_OK) return rc;
@@ -353,9 +359,9 @@ int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, 
     const long long n_src = idx ? (long long)n_seq * S : n_rows;
     const int D = cache->head_dim, Hk = cache->n_heads;
     if (!head_rows_ok(Hk, D, k_stride, n_src > 1 ? 2 : 1) || !head_rows_ok(Hk, D, v_stride, n_src > 1 ? 2 : 1)) return DART_ERR_BAD_SHAPE;
-    rc = check_rope(rope, D, n_rows, false);
+    rc = check_rope(rope, pos, pos_stride, D, n_rows, false);
     if (rc != DART_OK) return rc;
-    if (rope && rope->rot_dim && !rope->pos && rope->n_axes > 1) return DART_ERR_NULL; // a slot is a position on one axis only
+    if (rope && rope->rot_dim && !pos && rope->n_axes > 1) return DART_ERR_NULL; // a slot is a position on one axis only
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_weight, 16) || misaligned(cu_rows, 4) || misaligned(idx, 4) || misaligned(table, 4) ||
         misaligned(start, 4) || misaligned(status, 4))
         return DART_ERR_ALIGN;
@@ -370,7 +376,7 @@ int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, 
     p.side[0] = {(const char *)k, (char *)cache->k, (const char *)k_weight, 2 * k_stride, 0, Hk, true};
     p.side[1] = {(const char *)v, (char *)cache->v, nullptr, 2 * v_stride, 0, Hk, false};
     p.n_rows = n_rows, p.D = D, p.eps = eps;
-    set_rope(p, rope);
+    set_rope(p, rope, pos, pos_stride);
     p.n_seq = n_seq, p.per_seq = cu_rows ? 0 : n_rows / n_seq, p.S = S, p.table_stride = table_stride, p.page_size = cache->page_size;
     p.n_pages = cache->n_pages, p.cu = cu_rows, p.idx = idx, p.table = table, p.start = start, p.status = status;
     return cache->dtype == DART_BF16 ? launch_rows<__nv_bfloat16, true>(p, (cudaStream_t)stream) : launch_rows<__half, true>(p, (cudaStream_t)stream);

@@ -59,8 +59,7 @@ class dart_debug(ctypes.Structure):
 
 
 class dart_rope(ctypes.Structure):
-    _fields_ = [("inv_freq", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64),
-                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
                 ("section", ctypes.c_int32 * 3)]
 
 
@@ -119,9 +118,9 @@ def lib() -> ctypes.CDLL:
         L.dart_gather_rows.argtypes = [vp, i32p, i32, i32, i32, i32, vp, i32, vp]
         i64, f32 = ctypes.c_int64, ctypes.c_float
         L.dart_norm_rope.argtypes = [vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, f32, ctypes.POINTER(dart_rope), vp, i64,
-                                     vp, i64, i32, vp]
+                                     vp, i64, vp, i64, i32, vp]
         L.dart_cache_append.argtypes = [ctypes.POINTER(dart_cache), vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, i32, vp, vp, f32,
-                                        ctypes.POINTER(dart_rope), vp, vp]
+                                        ctypes.POINTER(dart_rope), vp, i64, vp, vp]
         L.dart_attend_workspace.argtypes = [ctypes.POINTER(dart_cache), ctypes.POINTER(dart_attend_args)]
         L.dart_attend_workspace.restype = ctypes.c_size_t
         L.dart_attend.argtypes = [ctypes.POINTER(dart_cache), ctypes.POINTER(dart_attend_args), vp, ctypes.c_size_t, vp]
@@ -184,17 +183,17 @@ def dart_gather_rows(src, idx, B, S, S_out, row_bytes, out, device, stream) -> i
 
 
 def dart_norm_rope(q, q_stride, n_q_heads, k, k_stride, n_k_heads, n_rows, head_dim, dtype, q_weight, k_weight, eps,
-                   rope: Optional[dart_rope], q_out, qo_stride, k_out, ko_stride, device, stream) -> int:
+                   rope: Optional[dart_rope], pos, pos_stride, q_out, qo_stride, k_out, ko_stride, device, stream) -> int:
     """Norm of each head and position rotation of queries and keys (raw device pointers); see include/dart.h."""
     return lib().dart_norm_rope(q, q_stride, n_q_heads, k, k_stride, n_k_heads, n_rows, head_dim, dtype, q_weight, k_weight,
-                                eps, rope, q_out, qo_stride, k_out, ko_stride, device, stream)
+                                eps, rope, pos, pos_stride, q_out, qo_stride, k_out, ko_stride, device, stream)
 
 
 def dart_cache_append(cache: Optional[dart_cache], k, k_stride, v, v_stride, n_seq, n_rows, cu_rows, idx, S, table, table_stride,
-                      start, k_weight, eps, rope: Optional[dart_rope], status, stream) -> int:
+                      start, k_weight, eps, rope: Optional[dart_rope], pos, pos_stride, status, stream) -> int:
     """Rows of keys and values into the pages of a cache (raw device pointers); see include/dart.h."""
     return lib().dart_cache_append(cache, k, k_stride, v, v_stride, n_seq, n_rows, cu_rows, idx, S, table, table_stride, start,
-                                   k_weight, eps, rope, status, stream)
+                                   k_weight, eps, rope, pos, pos_stride, status, stream)
 
 
 def dart_attend_workspace(cache: Optional[dart_cache], args: Optional[dart_attend_args]) -> int:
@@ -324,6 +323,48 @@ class Dart:
 
 
 # ---- around the reduction: rotated rows, the paged cache -------------------------------------------
+# (One token of a few sequences takes the GPU 3 us: the checks below ask a tensor for as little as they can.)
+
+_CODES = {}      # torch dtypes -> DART_*
+_raw_stream = None
+
+
+def _with_torch():
+    """torch, once: the current stream of a device as a number, and the types that rows may have."""
+    global _raw_stream
+    import torch
+
+    _CODES.update({torch.bfloat16: DART_BF16, torch.float16: DART_FP16})
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return torch
+
+
+def _code(dtype):
+    if not _CODES:
+        _with_torch()
+    if dtype not in _CODES:
+        raise ValueError("rows must be bf16 or fp16")
+    return _CODES[dtype]
+
+
+def _head_rows(t, name, dtype, device, n_rows, D):
+    """Rows [n_rows, heads, D] with the heads of a row side by side -> (address, values from row to row, heads)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.dtype is not dtype or t.device != device or shape[0] != n_rows or shape[2] != D:
+        raise ValueError("%s must be [%d rows, heads, %d] of type %s on %s" % (name, n_rows, D, dtype, device))
+    h = shape[1]
+    if (stride[2] != 1 and D > 1) or (stride[1] != D and h > 1):
+        raise ValueError("%s: the heads of a row must lie side by side" % name)
+    return t.data_ptr(), stride[0] if n_rows > 1 else h * D, h
+
+
+def _vector(t, name, size, dtype, device):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or t.shape != (size,) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d values of type %s on %s" % (name, size, dtype, device))
+    return t.data_ptr()
+
 
 class Rope:
     """A position rotation: the first ``2 * len(inv_freq)`` elements of a head turn by ``pos * inv_freq``, pairs being
@@ -335,89 +376,60 @@ class Rope:
 
         if not (inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()):
             raise ValueError("inv_freq must be a contiguous fp32 CUDA vector")
-        self.inv_freq, self.axes = inv_freq, len(sections) if sections is not None else 1
+        self.inv_freq, self.axes, self.device = inv_freq, len(sections) if sections is not None else 1, inv_freq.device
         if not 1 <= self.axes <= 3:
             raise ValueError("one to three sections")
-        self._c = (inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved), self.axes,
-                   tuple(int(n) for n in sections) + (0,) * (3 - self.axes) if sections is not None else (0, 0, 0))
+        self._int64 = torch.int64
+        self._c = dart_rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved), self.axes,
+                            tuple(int(n) for n in sections) + (0,) * (3 - self.axes) if sections is not None else (0, 0, 0))
 
     def at(self, pos, n_rows, device):
-        """The C struct for rows at ``pos`` ([n_rows], or [axes, n_rows]; None where the callee has its own)."""
-        import torch
-
-        inv_freq, rot_dim, interleaved, axes, section = self._c
-        if device != self.inv_freq.device:
+        """(struct, address, stride) for rows at ``pos`` ([n_rows], or [axes, n_rows]; None where the callee has its own)."""
+        if device != self.device:
             raise ValueError("inv_freq and the rows must be on the same device")
-        stride = 0
-        if pos is not None:
-            if not (pos.dtype == torch.int64 and pos.device == device and pos.numel() == axes * n_rows
-                    and pos.shape[-1] == n_rows and (n_rows <= 1 or pos.stride(-1) == 1)):
-                raise ValueError("pos must be int64 [%s%d] on the rows' device" % ("%d, " % axes if axes > 1 else "", n_rows))
-            stride = pos.stride(0) if axes > 1 else n_rows
-        return dart_rope(inv_freq, pos.data_ptr() if pos is not None else None, stride, rot_dim, interleaved, axes, section)
+        if pos is None:
+            return self._c, None, 0
+        shape, stride = pos.shape, pos.stride()
+        if (pos.dtype is not self._int64 or pos.device != device or shape[-1] != n_rows or (n_rows > 1 and stride[-1] != 1)
+                or (shape[0] if len(shape) == 2 else 1) != self.axes or not 1 <= len(shape) <= 2):
+            raise ValueError("pos must be int64 [%s%d] on the rows' device" % ("%d, " % self.axes if self.axes > 1 else "", n_rows))
+        return self._c, pos.data_ptr(), stride[0] if self.axes > 1 else n_rows
 
 
-def _dtype_code(dtype):
-    import torch
-
-    if dtype == torch.bfloat16:
-        return DART_BF16
-    if dtype == torch.float16:
-        return DART_FP16
-    raise ValueError("rows must be bf16 or fp16")
-
-
-def _head_rows(t, name, dtype, device, n_rows=None):
-    """[rows, heads, D] with the heads of a row side by side -> values from row to row."""
-    if t.dim() != 3 or t.dtype != dtype or t.device != device or not t.is_cuda or (n_rows is not None and t.shape[0] != n_rows):
-        raise ValueError("%s must be a CUDA tensor [rows, heads, head_dim] of the same type, device and rows as the others" % name)
-    n, h, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
-        raise ValueError("%s: the heads of a row must lie side by side" % name)
-    return t.stride(0) if n > 1 else h * d
-
-
-def _vector(t, name, size, dtype, device):
-    if t is not None and not (t.dtype == dtype and t.device == device and t.shape == (size,) and t.is_contiguous()):
-        raise ValueError("%s must be a contiguous vector of %d values of type %s on %s" % (name, size, dtype, device))
-    return t.data_ptr() if t is not None else None
-
-
-def _stream(stream, device):
-    import torch
-
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+_NO_ROPE = (None, None, 0)
+_NO_ROWS = (None, 0, 0)
 
 
 def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, out=None, stream=None):
     """Norm of each head (``q_weight`` / ``k_weight`` [D], None: no norm) and rotation of queries [N, Hq, D] and keys [N, Hk, D]
     (either may be None) in one pass.  ``pos``: int64 [N], or [axes, N].  ``out``: (q_out, k_out), which may be q and k
     themselves.  Returns (q_out, k_out)."""
-    import torch
-
     one = q if q is not None else k
     if one is None:
         raise ValueError("queries or keys are needed")
-    dtype, dev = one.dtype, one.device
-    code, n, D = _dtype_code(dtype), one.shape[0], one.shape[-1]
+    dtype, dev, shape = one.dtype, one.device, one.shape
+    code, index = _code(dtype), dev.index
+    if index is None:
+        raise ValueError("rows must be CUDA tensors")
+    n, D = shape[0], shape[-1]
     if out is None:
-        out = tuple(torch.empty(t.shape, dtype=dtype, device=dev) if t is not None else None for t in (q, k))
-    args = []
-    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
-        if t is None:
-            args.append((None, 0, 0, None, 0))
-            continue
-        stride = _head_rows(t, name, dtype, dev, n)
-        if t.shape[2] != D or o is None or o.shape != t.shape:
-            raise ValueError("%s: head_dim, or the shape of its output, differs" % name)
-        args.append((t.data_ptr(), stride, t.shape[1], o.data_ptr(), _head_rows(o, name + "_out", dtype, dev, n)))
-    (qp, qs, hq, qo, qos), (kp, ks, hk, ko, kos) = args
-    if rope is not None and pos is None:
+        out = tuple(t.new_empty(t.shape) if t is not None else None for t in (q, k))
+    q_out, k_out = out
+    qa = _head_rows(q, "q", dtype, dev, n, D) if q is not None else _NO_ROWS
+    ka = _head_rows(k, "k", dtype, dev, n, D) if k is not None else _NO_ROWS
+    qo = _head_rows(q_out, "q_out", dtype, dev, n, D) if q is not None else _NO_ROWS
+    ko = _head_rows(k_out, "k_out", dtype, dev, n, D) if k is not None else _NO_ROWS
+    if qo[2] != qa[2] or ko[2] != ka[2]:
+        raise ValueError("outputs must have the heads of their inputs")
+    if rope is None:
+        turn = _NO_ROPE
+    elif pos is None:
         raise ValueError("a rotation needs positions")
-    rc = lib().dart_norm_rope(qp, qs, hq, kp, ks, hk, n, D, code, _vector(q_weight, "q_weight", D, dtype, dev),
-                              _vector(k_weight, "k_weight", D, dtype, dev), eps,
-                              rope.at(pos, n, dev) if rope is not None else None, qo, qos, ko, kos, dev.index,
-                              _stream(stream, dev))
+    else:
+        turn = rope.at(pos, n, dev)
+    rc = lib().dart_norm_rope(qa[0], qa[1], qa[2], ka[0], ka[1], ka[2], n, D, code, _vector(q_weight, "q_weight", D, dtype, dev),
+                              _vector(k_weight, "k_weight", D, dtype, dev), eps, turn[0], turn[1], turn[2], qo[0], qo[1], ko[0], ko[1], index,
+                              stream.cuda_stream if stream is not None else _raw_stream(index))
     if rc != DART_OK:
         raise DartError(rc, "dart_norm_rope")
     return out
@@ -428,54 +440,56 @@ class PagedCache:
     number s lies in page ``table[sequence, s // page_size]``."""
 
     def __init__(self, k, v):
-        import torch
-
+        torch = _with_torch()
         if not (k.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device
                 and k.is_contiguous() and v.is_contiguous()):
             raise ValueError("k and v must be contiguous CUDA tensors [pages, heads, page_size, head_dim] of one type and device")
-        self.k, self.v = k, v
+        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self.heads, self.head_dim, self._index = k.shape[1], k.shape[3], k.device.index
         self._status = torch.zeros(4, dtype=torch.int32, device=k.device)
-        self._c = dart_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3], _dtype_code(k.dtype),
-                             k.device.index)
+        self._status_at, self._int32, self._torch = self._status.data_ptr(), torch.int32, torch
+        self._c = dart_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3], _code(k.dtype), self._index)
 
-    def _ints(self, t, name, shape=None):
-        import torch
-
+    def _ints(self, t, name, size=None):
         if t is None:
             return None
-        if not (t.dtype == torch.int32 and t.device == self.k.device and t.is_contiguous() and (shape is None or t.shape == shape)):
-            raise ValueError("%s must be contiguous int32%s on %s" % (name, " %s" % (tuple(shape),) if shape is not None else "", self.k.device))
+        if t.dtype is not self._int32 or t.device != self.device or not t.is_contiguous() or (size is not None and t.shape != (size,)):
+            raise ValueError("%s must be contiguous int32%s on %s" % (name, " [%d]" % size if size is not None else "", self.device))
         return t.data_ptr()
 
     def _table(self, t, name):
-        import torch
-
-        if not (t.dtype == torch.int32 and t.device == self.k.device and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1)
-                and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
-            raise ValueError("%s must be int32 [sequences, pages] on %s" % (name, self.k.device))
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is not self._int32 or t.device != self.device or len(shape) != 2 or (shape[1] > 1 and stride[1] != 1)
+                or (shape[0] > 1 and stride[0] < shape[1])):
+            raise ValueError("%s must be int32 [sequences, pages] on %s" % (name, self.device))
+        return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1], shape[0]
 
     def append(self, k, v, table, start=None, cu_rows=None, idx=None, S=0, pos=None, rope=None, k_weight=None, eps=1e-6, stream=None):
         """Rows of keys and values [N, heads, D] behind the ``start`` tokens that each sequence already has.  ``cu_rows``
         [sequences + 1]: ragged numbers of rows (None: equally many).  ``idx`` (a reduction's out_idx, flat or [B, S_out]): take row
         b * S + idx[n] for packed row n.  The keys are normalised (``k_weight``) and rotated (``rope``, at ``pos`` or at the slots)
         on the way."""
-        dev, dtype = self.k.device, self.k.dtype
-        _, heads, _, D = self.k.shape
-        ks, vs = _head_rows(k, "k", dtype, dev), _head_rows(v, "v", dtype, dev, k.shape[0])
-        n_seq, n = table.shape[0], k.shape[0] if idx is None else idx.numel()
-        if k.shape[1:] != (heads, D) or v.shape[1:] != (heads, D):
-            raise ValueError("k and v must have the cache's heads and head_dim")
-        if idx is not None and (S < 1 or k.shape[0] != n_seq * S):
-            raise ValueError("with idx, k and v hold S rows per sequence")
-        tp, ts = self._table(table, "table")
-        if pos is not None:
-            pos = pos.reshape(-1) if rope is not None and rope.axes == 1 else pos
-        rc = lib().dart_cache_append(self._c, k.data_ptr(), ks, v.data_ptr(), vs, n_seq, n, self._ints(cu_rows, "cu_rows", (n_seq + 1,)),
-                                     self._ints(idx, "idx"), S, tp, ts, self._ints(start, "start", (n_seq,)),
-                                     _vector(k_weight, "k_weight", D, dtype, dev), eps,
-                                     rope.at(pos, n, dev) if rope is not None else None, self._status.data_ptr(),
-                                     _stream(stream, dev))
+        dev, dtype, D = self.device, self.dtype, self.head_dim
+        tp, ts, n_seq = self._table(table, "table")
+        rows = k.shape[0]
+        ka, va = _head_rows(k, "k", dtype, dev, rows, D), _head_rows(v, "v", dtype, dev, rows, D)
+        if ka[2] != self.heads or va[2] != self.heads:
+            raise ValueError("k and v must have the cache's heads")
+        n = rows
+        if idx is not None:
+            n = idx.numel()
+            if S < 1 or rows != n_seq * S:
+                raise ValueError("with idx, k and v hold S rows per sequence")
+        if rope is None:
+            turn = _NO_ROPE
+        else:
+            if pos is not None and rope.axes == 1 and pos.dim() > 1:
+                pos = pos.reshape(-1)
+            turn = rope.at(pos, n, dev)
+        rc = lib().dart_cache_append(self._c, ka[0], ka[1], va[0], va[1], n_seq, n, self._ints(cu_rows, "cu_rows", n_seq + 1), self._ints(idx, "idx"),
+                                     S, tp, ts, self._ints(start, "start", n_seq), _vector(k_weight, "k_weight", D, dtype, dev), eps,
+                                     turn[0], turn[1], turn[2], self._status_at,
+                                     stream.cuda_stream if stream is not None else _raw_stream(self._index))
         if rc != DART_OK:
             raise DartError(rc, "dart_cache_append")
 
@@ -485,37 +499,33 @@ class PagedCache:
         lengths [groups], cu_group [groups + 1]) the tokens that a group of sequences shares.  ``cu_q`` [sequences + 1]: ragged
         numbers of rows (None: one row per sequence).  ``scale``: None for 1 / sqrt(D).  Returns ``out`` (made if None); ``lse``, a
         fp32 tensor [N, Hq], is filled if given."""
-        import torch
-
-        dev, dtype, D = self.k.device, self.k.dtype, self.k.shape[3]
-        if q.shape[-1] != D:
-            raise ValueError("q must have the cache's head_dim")
-        qs = _head_rows(q, "q", dtype, dev)
-        n, Hq, _ = q.shape
-        n_seq = table.shape[0]
-        on = torch.cuda.current_stream(dev)
-        with torch.cuda.stream(stream) if stream is not None and stream != on else contextlib.nullcontext():
-            if out is None:
-                out = torch.empty((n, Hq, D), dtype=dtype, device=dev)
-            elif out.shape != q.shape:
-                raise ValueError("out must have q's shape")
-            if lse is not None and not (lse.dtype == torch.float32 and lse.shape == (n, Hq) and lse.is_contiguous() and lse.device == dev):
-                raise ValueError("lse must be contiguous fp32 [rows, heads] on the rows' device")
-            tp, ts = self._table(table, "table")
-            groups, pp, ps, cg, pl = 0, None, 0, None, None
-            if prefix is not None:
-                groups = prefix[0].shape[0]
-                pp, ps = self._table(prefix[0], "prefix table")
-                pl, cg = self._ints(prefix[1], "prefix lengths", (groups,)), self._ints(prefix[2], "cu_group", (groups + 1,))
-            a = dart_attend_args(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, qs,
-                                 _head_rows(out, "out", dtype, dev, n), n, Hq, n_seq, groups, self._ints(cu_q, "cu_q", (n_seq + 1,)), tp,
-                                 self._ints(kv_len, "kv_len", (n_seq,)), cg, pp, pl, ts, ps, D ** -0.5 if scale is None else scale,
-                                 wait_limit, self._status.data_ptr())
-            L = lib()
-            # (made for this call on its stream: the allocator keeps it apart from other streams' and graphs' calls)
-            need = L.dart_attend_workspace(self._c, a)
-            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-            rc = L.dart_attend(self._c, a, ws.data_ptr() if ws is not None else None, need, (stream or on).cuda_stream)
+        if stream is not None: # (what is made below is made for that stream)
+            with self._torch.cuda.stream(stream):
+                return self.attend(q, table, kv_len, cu_q, prefix, scale, out, lse, wait_limit)
+        dev, dtype, D = self.device, self.dtype, self.head_dim
+        n = q.shape[0]
+        qa = _head_rows(q, "q", dtype, dev, n, D)
+        if out is None:
+            out = q.new_empty(q.shape)
+        oa = _head_rows(out, "out", dtype, dev, n, D)
+        if oa[2] != qa[2]:
+            raise ValueError("out must have q's heads")
+        if lse is not None and not (lse.dtype is self._torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == dev):
+            raise ValueError("lse must be contiguous fp32 [rows, heads] on the rows' device")
+        tp, ts, n_seq = self._table(table, "table")
+        if prefix is not None:
+            pp, ps, groups = self._table(prefix[0], "prefix table")
+            pl, cg = self._ints(prefix[1], "prefix lengths", groups), self._ints(prefix[2], "cu_group", groups + 1)
+        else:
+            pp, ps, groups, pl, cg = None, 0, 0, None, None
+        a = dart_attend_args(qa[0], oa[0], lse.data_ptr() if lse is not None else None, qa[1], oa[1], n, qa[2], n_seq, groups,
+                             self._ints(cu_q, "cu_q", n_seq + 1), tp, self._ints(kv_len, "kv_len", n_seq), cg, pp, pl, ts, ps,
+                             D ** -0.5 if scale is None else scale, wait_limit, self._status_at)
+        L = lib()
+        # (made for this call on its stream: the allocator keeps it apart from other streams' and graphs' calls)
+        need = L.dart_attend_workspace(self._c, a)
+        ws = self._torch.empty(need, dtype=self._torch.uint8, device=dev) if need else None
+        rc = L.dart_attend(self._c, a, ws.data_ptr() if need else None, need, _raw_stream(self._index))
         if rc != DART_OK:
             raise DartError(rc, "dart_attend")
         return out
@@ -523,9 +533,7 @@ class PagedCache:
     def status(self) -> int:
         """DART_OK, or what a kernel found wrong since the last reading (a page or an index out of range, a wait that gave up).
         Waits for the device; reading clears it."""
-        import torch
-
-        torch.cuda.synchronize(self.k.device)
+        self._torch.cuda.synchronize(self.device)
         code = int(self._status[0].item())
         if code:
             self._status.zero_()

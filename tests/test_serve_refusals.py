@@ -17,18 +17,17 @@ A, B, C, D_ = 1 << 20, 1 << 24, 1 << 28, 1 << 29  # addresses far apart
 
 
 def _rope(dart, **kw):
-    r = dict(inv_freq=A, pos=A, pos_stride=64, rot_dim=64, interleaved=0, n_axes=1, section=(0, 0, 0))
+    r = dict(inv_freq=A, rot_dim=64, interleaved=0, n_axes=1, section=(0, 0, 0))
     r.update(kw)
-    return dart.dart_rope(r["inv_freq"], r["pos"], r["pos_stride"], r["rot_dim"], r["interleaved"], r["n_axes"],
-                          (ctypes.c_int32 * 3)(*r["section"]))
+    return dart.dart_rope(r["inv_freq"], r["rot_dim"], r["interleaved"], r["n_axes"], (ctypes.c_int32 * 3)(*r["section"]))
 
 
 def _norm_rope(dart, **kw):
-    a = dict(q=A, qs=512, hq=4, k=B, ks=256, hk=2, n=8, D=128, dtype=0, wq=None, wk=None, eps=1e-6, rope=None, qo=C, qos=512, ko=D_,
-             kos=256)
+    a = dict(q=A, qs=512, hq=4, k=B, ks=256, hk=2, n=8, D=128, dtype=0, wq=None, wk=None, eps=1e-6, rope=None, pos=A, ps=64, qo=C, qos=512,
+             ko=D_, kos=256)
     a.update(kw)
     return dart.dart_norm_rope(a["q"], a["qs"], a["hq"], a["k"], a["ks"], a["hk"], a["n"], a["D"], a["dtype"], a["wq"], a["wk"], a["eps"],
-                               a["rope"], a["qo"], a["qos"], a["ko"], a["kos"], 0, None)
+                               a["rope"], a["pos"], a["ps"], a["qo"], a["qos"], a["ko"], a["kos"], 0, None)
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -45,12 +44,19 @@ def test_norm_rope_refuses(dart, kw, code):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(inv_freq=None), -1), (dict(pos=None), -1), (dict(rot_dim=8), -2), (dict(rot_dim=144), -2), (dict(rot_dim=-16), -2),
+    (dict(inv_freq=None), -1), (dict(rot_dim=8), -2), (dict(rot_dim=144), -2), (dict(rot_dim=-16), -2),
     (dict(n_axes=4), -2), (dict(n_axes=-1), -2), (dict(n_axes=3, section=(8, 8, 8)), -2), (dict(n_axes=3, section=(40, 8, -16)), -2),
-    (dict(n_axes=2, section=(16, 16, 0), pos_stride=7), -2), (dict(inv_freq=A + 2), -3), (dict(pos=A + 4), -3),
+    (dict(inv_freq=A + 2), -3),
 ])
 def test_rotations_that_are_refused(dart, kw, code):
     assert _norm_rope(dart, rope=_rope(dart, **kw)) == code
+
+
+def test_positions_that_are_refused(dart):
+    assert _norm_rope(dart, rope=_rope(dart), pos=None) == dart.DART_ERR_NULL
+    assert _norm_rope(dart, rope=_rope(dart), pos=A + 4) == dart.DART_ERR_ALIGN
+    assert _norm_rope(dart, rope=_rope(dart, n_axes=2, section=(16, 16, 0)), ps=7) == dart.DART_ERR_BAD_SHAPE
+    assert _norm_rope(dart, rope=_rope(dart, rot_dim=0), pos=None, n=0) == dart.DART_OK
 
 
 def test_columns_of_one_buffer_are_no_overlap(dart):
@@ -65,10 +71,10 @@ def test_columns_of_one_buffer_are_no_overlap(dart):
 def _append(dart, cache=None, **kw):
     c = dict(k=C, v=D_, n_pages=16, n_heads=2, page_size=16, head_dim=128, dtype=0, device=0)
     c.update(cache or {})
-    a = dict(k=A, ks=256, v=B, vs=256, n_seq=2, n=8, cu=None, idx=None, S=0, table=A, ts=4, start=None, wk=None, eps=1e-6, rope=None, status=None)
+    a = dict(k=A, ks=256, v=B, vs=256, n_seq=2, n=8, cu=None, idx=None, S=0, table=A, ts=4, start=None, wk=None, eps=1e-6, rope=None, pos=None, ps=0, status=None)
     a.update(kw)
     return dart.dart_cache_append(dart.dart_cache(*c.values()), a["k"], a["ks"], a["v"], a["vs"], a["n_seq"], a["n"], a["cu"], a["idx"], a["S"],
-                                  a["table"], a["ts"], a["start"], a["wk"], a["eps"], a["rope"], a["status"], None)
+                                  a["table"], a["ts"], a["start"], a["wk"], a["eps"], a["rope"], a["pos"], a["ps"], a["status"], None)
 
 
 @pytest.mark.parametrize("cache,kw,code", [
@@ -84,10 +90,10 @@ def test_append_refuses(dart, cache, kw, code):
 
 
 def test_append_takes_slots_as_positions_on_one_axis_only(dart):
-    assert _append(dart, rope=_rope(dart, pos=None, n_axes=3, section=(16, 8, 8))) == dart.DART_ERR_NULL
-    assert dart.dart_cache_append(None, A, 256, B, 256, 1, 1, None, None, 0, A, 1, None, None, 0.0, None, None, None) == dart.DART_ERR_NULL
+    assert _append(dart, rope=_rope(dart, n_axes=3, section=(16, 8, 8))) == dart.DART_ERR_NULL
+    assert dart.dart_cache_append(None, A, 256, B, 256, 1, 1, None, None, 0, A, 1, None, None, 0.0, None, None, 0, None, None) == dart.DART_ERR_NULL
 
 
 def test_struct_layouts(dart):
-    assert ctypes.sizeof(dart.dart_rope) == 48 and dart.dart_rope.rot_dim.offset == 24 and dart.dart_rope.section.offset == 36
+    assert ctypes.sizeof(dart.dart_rope) == 32 and dart.dart_rope.rot_dim.offset == 8 and dart.dart_rope.section.offset == 20
     assert ctypes.sizeof(dart.dart_cache) == 40 and dart.dart_cache.n_pages.offset == 16
