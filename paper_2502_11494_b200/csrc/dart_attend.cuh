@@ -24,6 +24,14 @@ namespace attend {
 constexpr int kErrCheck = -8;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// Division by a number that the host knows, for n < 2^31: a multiplication and a shift (Granlund and Montgomery's method: with
+// 2^(s-1) < d <= 2^s and m = ceil(2^(32+s) / d) - 2^32, n / d = (mulhi(n, m) + n) >> s).  A division takes some thirty instructions, and a 64-bit one is a call;
+// what a call of one token waits for is code that runs once.
+struct Divisor {
+    uint32_t m, s;
+    __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+};
+
 // Partial results by row and head: [rows][Hq][D] and [rows][Hq] (maximum in log2 units, sum).
 struct Whole {
     float *o;
@@ -43,6 +51,7 @@ struct Pieces {
     float2 *ml;      // [workers][2][M]
     Open *open;      // [workers] the item whose first piece, but not the last, is the worker's
     int M, n_workers; // rows of a tile
+    Divisor by_M;
 };
 
 struct Params {
@@ -54,10 +63,11 @@ struct Params {
     int n_rows, Hq, Hk, R, n_seq, n_groups, n_pages, page_shift;
     int table_stride, ptable_stride;
     const int32_t *cu_q, *table, *kv_len, *cu_group, *ptable, *plen;
+    Divisor by_R, by_Hk;
     float scale_log2;               // scale / ln 2: exponentials are powers of two
     int32_t *status;                // 4 words
     int n_prefix, n_own;            // segments of this launch: prefixes first
-    int n_workers, min_tiles, max_items;
+    int n_workers, max_items;
     Pieces pieces;
     Whole whole[2];                 // [0] prefixes, [1] own tokens
 };
@@ -92,7 +102,7 @@ __device__ inline Seg load_seg(const Params &p, int s)
         if (p.status) *p.status = kErrCheck;
         g.len = g.len < 0 ? 0 : (int)most;
     }
-    g.nmb = g.prefix && g.len == 0 ? 0 : (int)(((long long)g.n_q * p.R + p.pieces.M - 1) / p.pieces.M);
+    g.nmb = g.prefix && g.len == 0 ? 0 : p.pieces.by_M.of(g.n_q * p.R + p.pieces.M - 1);
     return g;
 }
 
@@ -102,7 +112,7 @@ __device__ __forceinline__ int sees(const Seg &g, int t) { return g.prefix ? g.l
 // writes their zeros).
 __device__ __forceinline__ int tile_sees(const Params &p, const Seg &g, int mb)
 {
-    return g.prefix ? g.len : sees(g, (min((mb + 1) * p.pieces.M, g.n_q * p.R) - 1) / p.R);
+    return g.prefix ? g.len : sees(g, p.by_R.of(min((mb + 1) * p.pieces.M, g.n_q * p.R) - 1));
 }
 template <int kTile>
 __device__ __forceinline__ int tiles_of(const Params &p, const Seg &g, int mb)
@@ -125,12 +135,24 @@ struct Start {
     long long off; // of the segment's room before the worker's share
 };
 
+__device__ __noinline__ long long div_long(long long a, long long b) { return a / b; }
+__device__ __forceinline__ long long div_of(long long a, long long b)
+{
+    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : div_long(a, b);
+}
+// Shares of the line: every worker's `each`, the first `more` of them one more.
+struct Shares {
+    long long each, more;
+    __device__ __forceinline__ long long first(long long w) const { return each * w + min(w, more); }
+    __device__ __forceinline__ long long size(int w) const { return each + (w < more); }
+};
+
 template <int kWorkers>
 struct PlanShared {
     Start start[kWorkers];
     long long tiles[32];
     int items[32];
-    long long n_tiles;
+    Shares shares;
 };
 
 // Every CTA finds where its workers begin.  Block-wide; ends with a barrier.
@@ -165,18 +187,19 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
     long long tb = t_sum - tiles;
     const bool ok = i_all <= p.max_items;
     if (tid < kWorkers) sh.start[tid] = Start{0, 0, 0};
+    Shares shares;
+    shares.each = ok ? div_of(t_all, p.n_workers) : 0, shares.more = ok ? t_all - shares.each * p.n_workers : 0;
     if (tid == 0) {
-        sh.n_tiles = ok ? t_all : 0;
+        sh.shares = shares;
         if (!ok && p.status) *p.status = kErrCheck;
     }
-    const int active = (int)min((long long)p.n_workers, max(1ll, t_all / p.min_tiles));
     __syncthreads();
     if (ok && t_all > 0)
 #pragma unroll 1
         for (int i = 0; i < kWorkers; ++i) {
             const long long w = (long long)blockIdx.x * kWorkers + i;
-            const long long at = t_all * w / active;
-            if (w >= active || at < tb || at >= tb + tiles) continue;
+            const long long at = shares.first(w);
+            if (at < tb || at >= tb + tiles) continue;
             int base = ib;
             long long first = tb;
             for (int s = s0; s < s1; ++s) {
@@ -212,8 +235,7 @@ struct Walk {
     __device__ __forceinline__ void begin(const Params &p, const PlanShared<kWorkers> &sh, int local)
     {
         worker = blockIdx.x * kWorkers + local;
-        const int active = (int)min((long long)p.n_workers, max(1ll, sh.n_tiles / p.min_tiles));
-        left = worker < active ? sh.n_tiles * (worker + 1) / active - sh.n_tiles * worker / active : 0;
+        left = sh.shares.size(worker);
         done = left == 0;
         if (done) return;
         const Start st = sh.start[local];
@@ -224,7 +246,7 @@ struct Walk {
             done = true;
             return;
         }
-        hk = (int)(st.off / head), mb = 0;
+        hk = (int)div_of(st.off, head), mb = 0;
         long long off = st.off - hk * head;
         for (; mb < g.nmb - 1; ++mb) {
             nt = kCost + tiles_of<kTile>(p, g, mb);
@@ -437,14 +459,14 @@ __global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(con
         // query fragments, and how many tokens the thread's two rows see
         uint32_t qa[kK][4];
         int lim[2];
-        long long row_at[2]; // row * Hq + head
+        int row_n[2], row_h[2]; // packed row, head
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = w.mb * kNarrowM + (i ? r1 : r0);
             const bool real = (i ? r1 : r0) < rows;
-            const int t = real ? r / p.R : 0, h = w.hk * p.R + (real ? r - t * p.R : 0);
+            const int t = real ? p.by_R.of(r) : 0, h = w.hk * p.R + (real ? r - t * p.R : 0);
             lim[i] = real ? sees(w.g, t) : w.vis;
-            row_at[i] = (long long)(w.g.row0 + t) * p.Hq + h;
+            row_n[i] = w.g.row0 + t, row_h[i] = h;
             const uint32_t *q = reinterpret_cast<const uint32_t *>(p.q + (long long)(w.g.row0 + t) * p.q_stride + (long long)h * (D * 2)) + (c0 >> 1);
 #pragma unroll
             for (int kk = 0; kk < kK; ++kk) {
@@ -536,17 +558,17 @@ __global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(con
             if (r >= rows) continue;
             if (w.is_whole() && p.n_groups == 0) {
                 const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
-                const long long n = row_at[i] / p.Hq, h = row_at[i] - n * p.Hq;
-                uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + n * p.out_stride + h * (D * 2)) + (c0 >> 1);
+                uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + row_n[i] * p.out_stride + (long long)row_h[i] * (D * 2)) + (c0 >> 1);
 #pragma unroll
                 for (int d = 0; d < kN; ++d) dst[d * 4] = pack2<T>(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
-                if (p.lse && (lane & 3) == 0) p.lse[row_at[i]] = lse_of(m[i], l[i]);
+                if (p.lse && (lane & 3) == 0) p.lse[(long long)row_n[i] * p.Hq + row_h[i]] = lse_of(m[i], l[i]);
             } else {
                 float *dst;
                 float2 *ml;
                 if (w.is_whole()) {
                     const Whole &to = p.whole[w.g.prefix ? 0 : 1];
-                    dst = to.o + row_at[i] * D, ml = to.ml + row_at[i];
+                    const long long at = (long long)row_n[i] * p.Hq + row_h[i];
+                    dst = to.o + at * D, ml = to.ml + at;
                 } else {
                     const long long at = w.place() * kNarrowM + r;
                     dst = p.pieces.o + at * D, ml = p.pieces.ml + at;
@@ -631,7 +653,7 @@ __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, co
 #pragma unroll
             for (int d = 0; d < kPer; ++d) acc[d] += x.v[d] * wgt;
         }
-        const int t = (o.r0 + r) / p.R;
+        const int t = p.by_R.of(o.r0 + r);
         write_row<T, D>(p, o.row0 + t, o.hk * p.R + (o.r0 + r - t * p.R), acc, top, sum);
     }
 }
@@ -645,10 +667,9 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
     __shared__ float s_o[kWarps][D], s_sum[kWarps];
     const Params &p = j.p;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = kWarps > 1 ? warp : 0;
-    const long long id = kWarps > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + warp;
-    const int per_row = (p.Hq + heads - 1) / heads;
+    const unsigned id = kWarps > 1 ? blockIdx.x : blockIdx.x * 4 + warp, per_row = (unsigned)(p.Hq + heads - 1) / (unsigned)heads;
     wait_for_previous();
-    const int n = (int)(id / per_row), h0 = (int)(id - (long long)n * per_row) * heads, nh = min(heads, p.Hq - h0);
+    const int n = (int)(id / per_row), h0 = (int)(id - n * per_row) * heads, nh = min(heads, p.Hq - h0);
     if (n >= p.n_rows) return;
     int b = n;
     if (p.cu_q) {
@@ -664,7 +685,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         b = lo;
     }
     // the lane's head (lanes 0 .. nh - 1; the others look at the last one): its pieces of the prefix, and its own
-    const int h = h0 + min(lane, nh - 1), hk = h / p.R;
+    const int h = h0 + min(lane, nh - 1), hk = p.by_R.of(h);
     int cnt[2] = {0, 0}, first[2] = {0, 0}, row_in[2] = {0, 0}; // first < 0: one piece, by row
     bool here = true;
 #pragma unroll
@@ -690,8 +711,8 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         const Pieces &f = j.from[kind];
         const int seg = j.seg_off[kind] + s;
         if (f.item_base[j.n_seg[kind]] < 0) return;
-        const int base = f.item_base[seg], nmb = (f.item_base[seg + 1] - base) / p.Hk;
-        const int r = (n - row0) * p.R + (h - hk * p.R), mb = r / f.M;
+        const int base = f.item_base[seg], nmb = p.by_Hk.of(f.item_base[seg + 1] - base);
+        const int r = (n - row0) * p.R + (h - hk * p.R), mb = f.by_M.of(r);
         if (r < 0 || mb >= nmb) { // (offsets that do not ascend)
             here = false;
             continue;

@@ -143,7 +143,7 @@ __device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, i
     Share s;
     const int r0 = g.r0 + e * rows;
     s.rows = clamp(g.n_q * p.R - r0, 0, rows);
-    const int vis = s.rows == 0 ? 0 : sees(g, (r0 + s.rows - 1) / p.R);
+    const int vis = s.rows == 0 ? 0 : sees(g, p.by_R.of(r0 + s.rows - 1));
     s.tiles = max(0, min(g.b, (vis + kWideTile - 1) / kWideTile) - g.a);
     return s;
 }
@@ -436,9 +436,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             begin = w->a, end = w->b;
             if (end < 0) return;
             sr = share_of(p, *w, kPair ? e : 0, rows);
-            const int t0 = (w->r0 + off) / p.R;
+            const int t0 = p.by_R.of(w->r0 + off);
             n0 = w->row0 + t0;
-            lim = row < sr.rows ? sees(*w, t0 + row / p.R) : w->vis;
+            lim = row < sr.rows ? sees(*w, t0 + p.by_R.of(row)) : w->vis;
             if (sr.tiles > 0 && (warp & 3) == 0 && lane == 0) {
                 // rows behind the segment's last are whatever comes next: nobody reads what comes of them
                 const uint32_t bar = smem_u32(&sh.q_full[e]);

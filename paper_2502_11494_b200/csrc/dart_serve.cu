@@ -204,6 +204,13 @@ int check_attend(const dart_cache *c, const dart_attend_args *a)
     return DART_OK;
 }
 
+dart::attend::Divisor divisor(int d)
+{
+    uint32_t s = 0;
+    while ((1ull << s) < (unsigned)d) ++s;
+    return {(uint32_t)(((1ull << (32 + s)) + d - 1) / (unsigned)d - (1ull << 32)), s};
+}
+
 typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -256,7 +263,7 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     p.q = (const char *)a->q, p.out = (char *)a->out, p.lse = a->lse, p.q_stride = 2 * a->q_stride, p.out_stride = 2 * a->out_stride;
     p.k = (const char *)c->k, p.v = (const char *)c->v;
     p.n_rows = a->n_rows, p.Hq = a->n_q_heads, p.Hk = c->n_heads, p.R = a->n_q_heads / c->n_heads, p.n_seq = a->n_seq, p.n_groups = a->n_groups;
-    p.n_pages = c->n_pages;
+    p.n_pages = c->n_pages, p.by_R = divisor(p.R), p.by_Hk = divisor(p.Hk);
     while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
     p.table_stride = a->table_stride, p.ptable_stride = a->prefix_stride;
     p.cu_q = a->cu_q, p.table = a->table, p.kv_len = a->kv_len, p.cu_group = a->cu_group, p.ptable = a->prefix_table, p.plen = a->prefix_len;
@@ -268,8 +275,8 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     for (int i = 0; i < L.n; ++i) {
         const Launch &l = L.launch[i];
         p.n_prefix = l.prefix ? a->n_groups : 0, p.n_own = l.own ? a->n_seq : 0;
-        p.n_workers = l.n_workers, p.min_tiles = 1, p.max_items = l.max_items;
-        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), (Open *)(ws + l.open), l.M, l.n_workers};
+        p.n_workers = l.n_workers, p.max_items = l.max_items;
+        p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), (Open *)(ws + l.open), l.M, l.n_workers, divisor(l.M)};
         for (int k = 0; k < 2; ++k)
             if (k ? l.own : l.prefix) j.from[k] = p.pieces, j.seg_off[k] = k ? p.n_prefix : 0, j.n_seg[k] = l.n_seg;
         cudaError_t e;
