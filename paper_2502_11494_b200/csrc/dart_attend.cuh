@@ -119,105 +119,103 @@ __device__ __forceinline__ int tiles_of(const Params &p, const Seg &g, int mb)
 {
     return max(1, (tile_sees(p, g, mb) + kTile - 1) / kTile);
 }
-// A segment's part of the line, for one KV head.
+// A segment's part of the line.
 template <int kTile, int kCost>
-__device__ long long room_per_head(const Params &p, const Seg &g)
+__device__ long long room_of(const Params &p, const Seg &g)
 {
     if (g.nmb == 0) return 0;
-    if (g.prefix || g.nmb == 1) return (long long)g.nmb * (kCost + tiles_of<kTile>(p, g, 0));
-    long long n = 0;
-    for (int mb = 0; mb < g.nmb; ++mb) n += kCost + tiles_of<kTile>(p, g, mb);
-    return n;
+    long long n = (long long)g.nmb * (kCost + tiles_of<kTile>(p, g, 0));
+    if (!g.prefix && g.nmb > 1) {
+        n = 0;
+        for (int mb = 0; mb < g.nmb; ++mb) n += kCost + tiles_of<kTile>(p, g, mb);
+    }
+    return n * p.Hk;
 }
 
+// Where a worker begins, as the thread of the plan that comes by it leaves it.  (What a call of one token waits for is code that runs
+// once, as fast as its instructions are fetched: everything here is kept short.)
 struct Start {
-    int seg, item_base;
-    long long off; // of the segment's room before the worker's share
-};
-
-__device__ __noinline__ long long div_long(long long a, long long b) { return a / b; }
-__device__ __forceinline__ long long div_of(long long a, long long b)
-{
-    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : div_long(a, b);
-}
-// Shares of the line: every worker's `each`, the first `more` of them one more.
-struct Shares {
-    long long each, more;
-    __device__ __forceinline__ long long first(long long w) const { return each * w + min(w, more); }
-    __device__ __forceinline__ long long size(int w) const { return each + (w < more); }
+    Seg g;
+    int seg, item_base, hk, mb, from; // the item, and the place in its room
 };
 
 template <int kWorkers>
 struct PlanShared {
     Start start[kWorkers];
-    long long tiles[32];
-    int items[32];
-    Shares shares;
+    long long room[32], items[32];
+    int each, more; // shares of the line: every worker's `each`, the first `more` of them one more
 };
 
-// Every CTA finds where its workers begin.  Block-wide; ends with a barrier.
+// Every CTA finds where its workers begin.  Block-wide; ends with a barrier.  (The line's length is counted in 32 bits: 2^31 tiles would
+// be 300 TB of keys and values to read.)
 template <int kTile, int kCost, int kWorkers>
 __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, n_seg = p.n_prefix + p.n_own;
-    const int per = (n_seg + nt - 1) / nt, s0 = min(tid * per, n_seg), s1 = min(s0 + per, n_seg);
-    int items = 0;
-    long long tiles = 0;
+    const int per = n_seg <= nt ? 1 : (n_seg + nt - 1) / nt, s0 = min(tid * per, n_seg), s1 = min(s0 + per, n_seg);
+    long long items = 0, room = 0;
+    Seg g;
+#pragma unroll 1
     for (int s = s0; s < s1; ++s) {
-        const Seg g = load_seg(p, s);
-        items += p.Hk * g.nmb, tiles += p.Hk * room_per_head<kTile, kCost>(p, g);
+        g = load_seg(p, s);
+        items += p.Hk * (long long)g.nmb, room += room_of<kTile, kCost>(p, g);
     }
-    int i_sum = items;
-    long long t_sum = tiles;
-#pragma unroll
+    long long i_sum = items, r_sum = room;
+#pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
-        const int a = __shfl_up_sync(0xffffffffu, i_sum, o);
-        const long long b = __shfl_up_sync(0xffffffffu, t_sum, o);
-        if (lane >= o) i_sum += a, t_sum += b;
+        const long long a = __shfl_up_sync(0xffffffffu, i_sum, o), b = __shfl_up_sync(0xffffffffu, r_sum, o);
+        if (lane >= o) i_sum += a, r_sum += b;
     }
-    if (lane == 31) sh.items[warp] = i_sum, sh.tiles[warp] = t_sum;
+    if (lane == 31) sh.items[warp] = i_sum, sh.room[warp] = r_sum;
     __syncthreads();
-    int i_all = 0;
-    long long t_all = 0;
+    long long i_all = 0, r_all = 0;
+#pragma unroll 1
     for (int w = 0; w < nt / 32; ++w) {
-        if (w == warp) i_sum += i_all, t_sum += t_all;
-        i_all += sh.items[w], t_all += sh.tiles[w];
+        if (w == warp) i_sum += i_all, r_sum += r_all;
+        i_all += sh.items[w], r_all += sh.room[w];
     }
-    int ib = i_sum - items;
-    long long tb = t_sum - tiles;
-    const bool ok = i_all <= p.max_items;
-    if (tid < kWorkers) sh.start[tid] = Start{0, 0, 0};
-    Shares shares;
-    shares.each = ok ? div_of(t_all, p.n_workers) : 0, shares.more = ok ? t_all - shares.each * p.n_workers : 0;
+    const bool ok = i_all <= p.max_items && r_all < 0x7fffffffll;
+    const int each = ok ? (int)((unsigned)r_all / (unsigned)p.n_workers) : 0, more = ok ? (int)r_all - each * p.n_workers : 0;
     if (tid == 0) {
-        sh.shares = shares;
+        sh.each = each, sh.more = more;
         if (!ok && p.status) *p.status = kErrCheck;
     }
-    __syncthreads();
-    if (ok && t_all > 0)
+    if (ok && room > 0) {
+        const int begin = (int)(r_sum - room), end = (int)r_sum; // the thread's part of the line
 #pragma unroll 1
         for (int i = 0; i < kWorkers; ++i) {
-            const long long w = (long long)blockIdx.x * kWorkers + i;
-            const long long at = shares.first(w);
-            if (at < tb || at >= tb + tiles) continue;
-            int base = ib;
-            long long first = tb;
-            for (int s = s0; s < s1; ++s) {
-                const Seg g = load_seg(p, s);
-                const long long n = p.Hk * room_per_head<kTile, kCost>(p, g);
-                if (at < first + n) {
-                    sh.start[i] = Start{s, base, at - first};
+            const int w = blockIdx.x * kWorkers + i, at = each * w + min(w, more);
+            if (at < begin || at >= end) continue;
+            int base = (int)(i_sum - items), first = begin, s = s0;
+            for (;; ++s) { // (with one segment a thread it is at hand)
+                if (per > 1) g = load_seg(p, s);
+                const int n = per > 1 ? (int)room_of<kTile, kCost>(p, g) : (int)room;
+                if (at < first + n || s + 1 >= s1) {
+                    const int head = p.by_Hk.of(n), off = at - first;
+                    Start st;
+                    st.g = g, st.seg = s, st.item_base = base;
+                    st.hk = head > 0 ? (int)((unsigned)off / (unsigned)head) : 0;
+                    st.from = off - st.hk * head;
+                    for (st.mb = 0; st.mb < g.nmb - 1; ++st.mb) {
+                        const int in = kCost + tiles_of<kTile>(p, g, st.mb);
+                        if (st.from < in) break;
+                        st.from -= in;
+                    }
+                    sh.start[i] = st;
                     break;
                 }
                 first += n, base += p.Hk * g.nmb;
             }
         }
+    }
     if (blockIdx.x == 0) {
+        int base = (int)(i_sum - items);
+#pragma unroll 1
         for (int s = s0; s < s1; ++s) {
-            p.pieces.item_base[s] = ib;
-            ib += p.Hk * load_seg(p, s).nmb;
+            p.pieces.item_base[s] = base;
+            if (s + 1 < s1) base += p.Hk * load_seg(p, s).nmb;
         }
-        if (tid == 0) p.pieces.item_base[n_seg] = ok ? i_all : -1;
+        if (tid == 0) p.pieces.item_base[n_seg] = ok ? (int)i_all : -1;
     }
     __syncthreads();
 }
@@ -228,32 +226,18 @@ struct Walk {
     Seg g;
     int s, item_base, hk, mb, a, b, nt, vis, worker; // piece: tiles [a, b) of nt
     int from, to;                                    // ... and its place in the item's room
-    long long left;
+    int left;
     bool done;
 
     template <int kWorkers>
     __device__ __forceinline__ void begin(const Params &p, const PlanShared<kWorkers> &sh, int local)
     {
         worker = blockIdx.x * kWorkers + local;
-        left = sh.shares.size(worker);
+        left = sh.each + (worker < sh.more);
         done = left == 0;
         if (done) return;
-        const Start st = sh.start[local];
-        s = st.seg, item_base = st.item_base;
-        g = load_seg(p, s);
-        const long long head = room_per_head<kTile, kCost>(p, g);
-        if (head <= 0) { // (lengths that change under the kernel)
-            done = true;
-            return;
-        }
-        hk = (int)div_of(st.off, head), mb = 0;
-        long long off = st.off - hk * head;
-        for (; mb < g.nmb - 1; ++mb) {
-            nt = kCost + tiles_of<kTile>(p, g, mb);
-            if (off < nt) break;
-            off -= nt;
-        }
-        from = (int)off;
+        const Start &st = sh.start[local];
+        g = st.g, s = st.seg, item_base = st.item_base, hk = st.hk, mb = st.mb, from = st.from;
         piece(p);
         if (a == b) next(p); // (a share that ends before the item's first tile)
     }
@@ -261,7 +245,7 @@ struct Walk {
     {
         vis = tile_sees(p, g, mb);
         nt = tiles_of<kTile>(p, g, mb);
-        to = (int)min((long long)nt + kCost, from + left);
+        to = min(nt + kCost, from + left);
         a = max(0, from - kCost), b = max(0, to - kCost);
     }
     __device__ __forceinline__ void next(const Params &p)
