@@ -44,9 +44,10 @@ constexpr uint32_t kNoteFirst = 8, kNoteLast = 16, kNoteEnd = 1u << 31;
 
 // A piece as the softmax threads need it, written by the copying warp, which is ahead of them.
 struct PieceNote {
-    int row0, n_q, len, hk, r0; // its segment's rows and own tokens (prefix: all rows see all of them), its KV head, its first row
-    int a, b, vis, place;       // tiles; tokens that its last row sees; where its sums go: kToRows, or a place among the workers'
-    int prefix;                 // (b < 0: nothing follows)
+    int a, b, vis, place;                  // tiles (b < 0: nothing follows); tokens that its last row sees; where its sums go: kToRows, or a
+                                           // place among the workers'
+    int hk, len, prefix;                   // KV head; tokens of the segment
+    int n0[2], rows[2], tiles[2], sees[2]; // per engine: first packed row, rows, tiles, how many tokens its first row would see if len had no end
 };
 constexpr int kToRows = -1;
 
@@ -68,6 +69,35 @@ __device__ __forceinline__ void tma_queries(uint32_t dst, const CUtensorMap *tm,
                  "r"(0), "r"(hk), "r"(n), "r"(bar)
                  : "memory");
 }
+// Bounded waits that sleep: the hardware wakes a waiting warp when the phase ends, or after the hint (in ns), when it looks whether the
+// CTA has given up or its time is over.  (A warp that asks again and again takes issue slots from those that compute.)
+constexpr uint32_t kSleepNs = 20000;
+__device__ __forceinline__ bool asleep_until(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity), "r"(kSleepNs)
+                 : "memory");
+    return ok != 0;
+}
+struct Waits {
+    sweep::Ctl ctl;
+    __device__ bool wait_bar(uint32_t bar, uint32_t parity, int where, long long task) const
+    {
+        if (asleep_until(bar, parity)) return true;
+        const long long t0 = clock64();
+        while (!asleep_until(bar, parity)) {
+            if (ctl.aborted()) return false;
+            if ((unsigned long long)(clock64() - t0) > ctl.limit_cycles) {
+                ctl.give_up(where, task);
+                return false;
+            }
+        }
+        return true;
+    }
+    __device__ void wait_landed(uint32_t bar, uint32_t parity) const { ctl.wait_landed(bar, parity); }
+};
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t r;
@@ -134,18 +164,22 @@ __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t *r)
 }
 
 // An engine's part of a piece: its rows, and how many of the piece's tiles its last row sees anything of.
-struct Share {
-    int rows, tiles;
-};
-__device__ __forceinline__ int sees(const PieceNote &g, int t) { return g.prefix ? g.len : clamp(g.len - g.n_q + t + 1, 0, g.len); }
-__device__ __forceinline__ Share share_of(const Params &p, const PieceNote &g, int e, int rows)
+template <typename W>
+__device__ __forceinline__ PieceNote piece_note(const Params &p, const W &w, int engines, int rows)
 {
-    Share s;
-    const int r0 = g.r0 + e * rows;
-    s.rows = clamp(g.n_q * p.R - r0, 0, rows);
-    const int vis = s.rows == 0 ? 0 : sees(g, p.by_R.of(r0 + s.rows - 1));
-    s.tiles = max(0, min(g.b, (vis + kWideTile - 1) / kWideTile) - g.a);
-    return s;
+    PieceNote g;
+    g.a = w.a, g.b = w.b, g.vis = w.vis, g.place = w.is_whole() ? kToRows : (int)w.place();
+    g.hk = w.hk, g.len = w.g.len, g.prefix = w.g.prefix;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int r0 = w.mb * p.pieces.M + e * rows, t0 = p.by_R.of(r0);
+        g.n0[e] = w.g.row0 + t0;
+        g.rows[e] = e < engines ? clamp(w.g.n_q * p.R - r0, 0, rows) : 0;
+        const int vis = g.rows[e] == 0 ? 0 : sees(w.g, p.by_R.of(r0 + g.rows[e] - 1));
+        g.tiles[e] = max(0, min(w.b, (vis + kWideTile - 1) / kWideTile) - w.a);
+        g.sees[e] = w.g.prefix ? w.g.len : w.g.len - w.g.n_q + t0 + 1;
+    }
+    return g;
 }
 
 template <typename T, int D, bool kPair>
@@ -198,7 +232,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     wait_for_previous();
     plan<kWideTile, kWideCost, kWorkers>(p, *reinterpret_cast<PlanShared<kWorkers> *>(&sh.plan));
     const PlanShared<kWorkers> &pl = *reinterpret_cast<const PlanShared<kWorkers> *>(&sh.plan);
-    const sweep::Ctl ctl{&sh.abort, status, limit_cycles};
+    const Waits ctl{{&sh.abort, status, limit_cycles}};
 
     // The softmax threads hold a row of 128 scores: 216 registers; the others give theirs (256 x 216 + 128 x 72 = 384 x 168).
     if (warp >= 8)
@@ -232,7 +266,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 ++pieces;
             };
             for (; ok && !w.done; w.next(p)) {
-                const PieceNote piece{w.g.row0, w.g.n_q, w.g.len, w.hk, w.mb * p.pieces.M, w.a, w.b, w.vis, w.is_whole() ? kToRows : (int)w.place(), (int)w.g.prefix};
+                const PieceNote piece = piece_note(p, w, kPair ? 2 : 1, rows);
                 if (first) {
                     if (lane == 0) {
                         w.note(p);
@@ -251,14 +285,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     }
                     return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
                 };
-                const Share s0 = share_of(p, piece, 0, rows), s1 = kPair ? share_of(p, piece, 1, rows) : Share{0, 0};
                 int next_row = page_row(w.a);
                 for (int tile = w.a; ok && tile < w.b; ++tile) {
                     const int row = next_row;
                     next_row = page_row(tile + 1);
                     const int tokens = clamp(w.vis - tile * kWideTile, 0, kWideTile), n = (tokens + box - 1) / box, i_tile = tile - w.a;
-                    const uint32_t note = (i_tile < s0.tiles ? 1u : 0u) | (i_tile < s1.tiles ? 2u : 0u) | (i_tile == 0 ? kNoteFirst : 0u) |
-                                          (i_tile == s0.tiles - 1 ? kNoteLast : 0u) | (i_tile == s1.tiles - 1 ? 2 * kNoteLast : 0u) | (uint32_t)((tokens + 15) >> 4) << 8;
+                    const uint32_t note = (i_tile < piece.tiles[0] ? 1u : 0u) | (i_tile < piece.tiles[1] ? 2u : 0u) | (i_tile == 0 ? kNoteFirst : 0u) |
+                                          (i_tile == piece.tiles[0] - 1 ? kNoteLast : 0u) | (i_tile == piece.tiles[1] - 1 ? 2 * kNoteLast : 0u) | (uint32_t)((tokens + 15) >> 4) << 8;
 #pragma unroll 1
                     for (int i = k0; ok && i < k1; ++i) {
                         const uint32_t fill = 2 * tiles + i;
@@ -281,7 +314,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     ++tiles;
                 }
             }
-            if (first && ok) announce(PieceNote{0, 0, 0, 0, 0, 0, -1, 0, 0, 0});
+            if (first && ok) {
+                PieceNote none = {};
+                none.b = -1;
+                announce(none);
+            }
             if (first && ok && lane == 0) { // nothing follows
                 const uint32_t fill = 2 * tiles;
                 const int at = (int)(fill % kPlaces);
@@ -329,22 +366,37 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 }
                 __syncwarp();
             };
-            const auto sums = [&](int e, int at, uint32_t note) { // in halves of 64 tokens, as their weights come
-                const unsigned long long db = desc_v + (unsigned)(at * (kPlace >> 4));
+            // the sums of a tile, in halves of 64 tokens, as their weights come, and with the second one the scores of the next tile
+            // where its keys are there: twelve products on end
+            const auto sums = [&](int e, int at, uint32_t note, int at_next, bool more) {
+                const unsigned long long dv = desc_v + (unsigned)(at * (kPlace >> 4)), da = umma_desc(q_at(e)), db = desc + (unsigned)(at_next * (kPlace >> 4));
                 const int steps = (int)(note >> 8) & 15;
                 const uint32_t phase = n_p[e]++ & 1u, s_at = tmem + e * 256;
+                if (!wait(smem_u32(&sh.p_half[e]), phase, kWaitWeights)) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issues) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (!wait(smem_u32(h ? &sh.p_full[e] : &sh.p_half[e]), phase, kWaitWeights)) return false;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (issues) {
-#pragma unroll
-                        for (int kk = h * 4; kk < h * 4 + 4; ++kk) // (16 tokens on: 2048 bytes; 8 columns of weights)
-                            if (kk < steps) umma_ts(s_at + 128, s_at + kk * 8, db + kk * 128, id_o, kk > 0 || !(note & kNoteFirst));
-                        if (h && (note & (kPair ? kNoteLast << e : kNoteLast))) umma_commit(smem_u32(&sh.o_full[e]));
-                    }
-                    __syncwarp();
+                    for (int kk = 0; kk < 4; ++kk) // (16 tokens on: 2048 bytes; 8 columns of weights)
+                        if (kk < steps) umma_ts(s_at + 128, s_at + kk * 8, dv + kk * 128, id_o, kk > 0 || !(note & kNoteFirst));
                 }
+                __syncwarp();
+                if (!wait(smem_u32(&sh.p_full[e]), phase, kWaitWeights)) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issues) {
+#pragma unroll
+                    for (int kk = 4; kk < 8; ++kk)
+                        if (kk < steps) umma_ts(s_at + 128, s_at + kk * 8, dv + kk * 128, id_o, 1u);
+                    if (note & (kPair ? kNoteLast << e : kNoteLast)) umma_commit(smem_u32(&sh.o_full[e]));
+                    if (more) {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const int off = (kk >> 2) * (kHalf >> 4) + (kk & 3) * 2;
+                            umma_ss(s_at, da + off, db + off, id_s, kk != 0);
+                        }
+                        umma_commit(smem_u32(&sh.s_full[e]));
+                    }
+                }
+                __syncwarp();
                 return true;
             };
             const auto release = [&](int at) { // when all products so far have ended
@@ -382,15 +434,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 const bool ready = __all_sync(0xffffffffu, sweep::mbar_try_wait(full + at * 8, round)) != 0;
                 uint32_t next = ready ? sh.note[ring][at] : kNoteFirst;
                 const bool along = !(next & (kNoteFirst | kNoteEnd)); // (where a piece ends the engines do not wait for each other's end)
-                if (kPair) {
-                    if (note & 1u) ok = sums(0, at_v, note);
-                    if (ok && along && (next & 1u)) scores(0, at);
-                    if (ok && (note & 2u)) ok = sums(1, at_v, note);
-                    if (ok && along && (next & 2u)) scores(1, at);
-                } else if (note & 1u) {
-                    ok = sums(ring, at_v, note);
-                    if (ok && along && (next & 1u)) scores(ring, at);
-                }
+                if (note & 1u) ok = sums(ring, at_v, note, at, along && (next & 1u));
+                if (kPair && ok && (note & 2u)) ok = sums(1, at_v, note, at, along && (next & 2u));
                 if (!ok) break;
                 release(at_v);
                 if (!ready) {
@@ -420,12 +465,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         const int e = warp >> 2, ring = kPair ? 0 : e, row = (warp & 3) * 32 + lane;
         const uint32_t s_at = tmem + e * 256 + ((uint32_t)((warp & 3) * 32) << 16), o_at = s_at + 128;
         const uint32_t stage = base + (uint32_t)(2 + kWorkers * kPlaces) * kPlace + warp * 4096;
-        const int off = kPair ? e * rows : 0;                        // of the engine's first row
+        const int en = kPair ? e : 0, off = kPair ? e * rows : 0;  // the engine's part of a note; its first row
+        const uint32_t inv_R = (65536u + p.R - 1) / (uint32_t)p.R; // row / R for rows below 128: (row * inv_R) >> 16
         uint32_t seen = 0, n_s = 0, n_o = 0, pieces = 0; // tiles of the ring passed so far; phases
         bool ok = true;
         const PieceNote *w = &sh.piece[ring][0]; // (read where it is wanted: registers are for scores)
-        Share sr{0, 0};
-        int n0 = 0, lim = 0, begin = 0, end = -1; // the engine's first packed row; how many tokens the thread's row sees; the piece's tiles
+        int my_rows = 0, my_tiles = 0, n0 = 0, lim = 0, begin = 0, end = -1; // the engine's rows, tiles and first packed row; tokens that the
+                                                                             // thread's row sees; the piece's tiles
         // The next piece, and its queries: the scores of the piece before are all there, so that nobody reads its queries any more.
         const auto next_piece = [&]() {
             const int at = (int)(pieces % kPieces);
@@ -435,11 +481,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             ++pieces;
             begin = w->a, end = w->b;
             if (end < 0) return;
-            sr = share_of(p, *w, kPair ? e : 0, rows);
-            const int t0 = p.by_R.of(w->r0 + off);
-            n0 = w->row0 + t0;
-            lim = row < sr.rows ? sees(*w, t0 + p.by_R.of(row)) : w->vis;
-            if (sr.tiles > 0 && (warp & 3) == 0 && lane == 0) {
+            my_rows = w->rows[en], my_tiles = w->tiles[en], n0 = w->n0[en];
+            lim = row >= my_rows ? w->vis : w->prefix ? w->len : clamp(w->sees[en] + (int)(row * inv_R >> 16), 0, w->len);
+            if (my_tiles > 0 && (warp & 3) == 0 && lane == 0) {
                 // rows behind the segment's last are whatever comes next: nobody reads what comes of them
                 const uint32_t bar = smem_u32(&sh.q_full[e]);
                 mbar_arrive_expect_tx(bar, (uint32_t)(rows * D * 2));
@@ -450,7 +494,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         next_piece();
         while (ok && end >= 0) {
             float m = -INFINITY, l = 0.0f;
-            for (int tile = begin; ok && tile < begin + sr.tiles; ++tile) {
+            for (int tile = begin; ok && tile < begin + my_tiles; ++tile) {
                 ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.s_full[e]), n_s & 1u, kWaitScores, pieces));
                 if (!ok) break;
                 ++n_s;
@@ -479,7 +523,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
                 for (int i = 4; i < 128; i += 4) t0 = fmaxf(t0, s[i]), t1 = fmaxf(t1, s[i + 1]), t2 = fmaxf(t2, s[i + 2]), t3 = fmaxf(t3, s[i + 3]);
                 const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * p.scale_log2;
-                if (__any_sync(0xffffffffu, row < sr.rows && top > m + 8.0f)) { // (from -inf: any; rows of nobody hold whatever was there)
+                if (__any_sync(0xffffffffu, row < my_rows && top > m + 8.0f)) { // (from -inf: any; rows of nobody hold whatever was there)
                     const float now = fmaxf(m, top), fix = m == now ? 1.0f : exp2_approx(m - now);
                     if (tile > begin) { // (this tile's scores being there, the products before them have ended)
 #pragma unroll 1
@@ -521,9 +565,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             if (!ok) break;
             seen += end - begin;
             // what the piece leaves, and where; then, while its last products run, the next one's queries are asked for
-            const Share had = sr;
-            const uint32_t inv_R = (65536u + p.R - 1) / (uint32_t)p.R; // row / R for rows below 128: (row * inv_R) >> 16
-            const int my_t = (int)(row * inv_R >> 16), my_h = row - my_t * p.R;
+            const int had_rows = my_rows, had_tiles = my_tiles, my_t = (int)(row * inv_R >> 16), my_h = row - my_t * p.R;
             const bool by_row = w->place == kToRows, at_once = by_row && p.n_groups == 0;
             const int h0 = w->hk * p.R;
             char *dst;             // of the engine's first row; the next token's and the next head's are so far on
@@ -535,7 +577,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 per_t = (long long)(by_row ? p.Hq : p.R) * (D * 4), per_h = D * 4;
                 dst = (char *)(by_row ? p.whole[w->prefix ? 0 : 1].o : p.pieces.o) + (by_row ? (long long)n0 * p.Hq + h0 : (long long)w->place * p.pieces.M + off) * (D * 4);
             }
-            if (row < had.rows) {
+            if (row < had_rows) {
                 const long long at = by_row ? (long long)(n0 + my_t) * p.Hq + h0 + my_h : (long long)w->place * p.pieces.M + off + row;
                 if (!at_once)
                     (by_row ? p.whole[w->prefix ? 0 : 1].ml : p.pieces.ml)[at] = make_float2(m, l);
@@ -546,13 +588,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             if (lane == 0) mbar_arrive(smem_u32(&sh.piece_empty[ring][(pieces - 1) % kPieces]));
             next_piece();
             if (!ok) break;
-            if (had.tiles > 0) {
+            if (had_tiles > 0) {
                 ok = __all_sync(0xffffffffu, ctl.wait_bar(smem_u32(&sh.o_full[e]), n_o & 1u, kWaitSums, pieces));
                 if (!ok) break;
                 ++n_o;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            if (had.tiles == 0 && !at_once) continue; // (where l is 0 nobody reads the sums)
+            if (had_tiles == 0 && !at_once) continue; // (where l is 0 nobody reads the sums)
             // Rows go out by way of shared memory, 128 bytes of 32 rows at a time, so that a store fills whole lines (a thread that
             // writes its own row keeps the load-store unit for 32 lines an instruction: a piece took 17000 cycles beside its tiles).
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -568,7 +610,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     const int in_warp = i * 4 + (lane >> 3), r = (warp & 3) * 32 + in_warp, piece = lane & 7;
                     const int t = (int)(r * inv_R >> 16), hh = r - t * p.R;
                     const uint4 x = sweep::lds128(stage + in_warp * 128 + ((piece ^ (in_warp & 7)) << 4));
-                    if (r < had.rows) *reinterpret_cast<uint4 *>(dst + t * per_t + hh * per_h + c + piece * 16) = x;
+                    if (r < had_rows) *reinterpret_cast<uint4 *>(dst + t * per_t + hh * per_h + c + piece * 16) = x;
                 }
                 __syncwarp();
             };
@@ -577,7 +619,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 for (int c = 0; c < D; c += 64) {
                     float o[64];
                     uint32_t v[32];
-                    if (had.tiles > 0) {
+                    if (had_tiles > 0) {
                         tmem_ld32(o_at + c, o), tmem_ld32(o_at + c + 32, o + 32);
                         tmem_wait_ld();
                     }
