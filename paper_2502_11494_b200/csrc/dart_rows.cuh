@@ -20,7 +20,7 @@
 namespace dart {
 namespace rows {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kMaxRows = 8;      // rows per block
 constexpr int kMaxHalf = 128;    // rotated pairs of a head (head_dim <= 256)
 constexpr int kErrCheck = -8;    // status: an index or a page outside its range
@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(kThreads) head_rows_kernel(const Params p)
     const int row0 = blockIdx.x * p.rows_per_block, n_here = min(p.rows_per_block, p.n_rows - row0);
     const int H = p.side[0].heads + p.side[1].heads;
     const int h0 = blockIdx.y * p.heads_per_block, nh = min(p.heads_per_block, H - h0);
+    const float inv_D = 1.0f / (float)p.D;
     wait_for_previous();
     if (kPaged) {
         if (tid < n_here) s_place[tid] = place_of(p, row0 + tid);
@@ -166,8 +167,8 @@ __global__ void __launch_bounds__(kThreads) head_rows_kernel(const Params p)
         const long long src = kPaged ? s_place[r].src : row0 + r;
         if (src < 0) return;
         const uint4 *at = reinterpret_cast<const uint4 *>(s.src + src * s.src_stride) + (long long)(h0 + hh - (second ? p.side[0].heads : 0)) * pieces;
-        if (has0) w0 = at[c0];
-        if (has1) w1 = at[c1];
+        if (has0) w0 = ld_stream<true>(at + c0);
+        if (has1) w1 = ld_stream<true>(at + c1);
     };
     fetch(row, h);
 
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) head_rows_kernel(const Params p)
         }
         if (here && (norm || turn)) {
             if (norm) {
-                const float scale = 1.0f / sqrtf(ss / (float)p.D + p.eps);
+                const float scale = rsqrtf(ss * inv_D + p.eps);
                 float u[8];
                 const uint4 *w = reinterpret_cast<const uint4 *>(s.weight);
                 if (has0) {
@@ -260,8 +261,8 @@ __global__ void __launch_bounds__(kThreads) head_rows_kernel(const Params p)
                 at = s.dst + (((s_place[r].page * s.heads + head) * p.page_size + s_place[r].at) * (long long)p.D) * 2;
             else
                 at = s.dst + (row0 + r) * s.dst_stride + (long long)head * p.D * 2;
-            if (has0) reinterpret_cast<uint4 *>(at)[c0] = out0;
-            if (has1) reinterpret_cast<uint4 *>(at)[c1] = out1;
+            if (has0) st_stream(reinterpret_cast<uint4 *>(at) + c0, out0);
+            if (has1) st_stream(reinterpret_cast<uint4 *>(at) + c1, out1);
         }
     }
 }

@@ -58,8 +58,9 @@ void set_rope(dart::rows::Params &p, const dart_rope *r, const int64_t *pos, int
 bool known_type(int dtype) { return dtype == DART_BF16 || dtype == DART_FP16; }
 bool head_rows_ok(int heads, int D, long long stride, int n_rows) { return heads >= 0 && (n_rows <= 1 || stride >= (long long)heads * D) && stride % 8 == 0 && stride >= 0; }
 
-// Blocks of 256 threads.  Few rows: one round of heads per block, a row's heads over several blocks.  Many rows: up to eight rows
-// a block, so that a thread has several rounds to overlap and the rows' angles serve all heads.
+// Few rows: one round of heads per block, a row's heads over several blocks.  Many rows: up to eight rows a block, so that a thread has
+// several rounds to overlap and the rows' angles serve all heads (43264 rows of 64 heads of 128: eight rounds 235 us, four 246, sixteen 235;
+// blocks of 256 threads 246, of 64 230, but 4 % slower on 18832 rows of 32 heads with sixteen rounds).
 template <typename T, bool kPaged>
 int launch_rows(dart::rows::Params &p, cudaStream_t st)
 {
