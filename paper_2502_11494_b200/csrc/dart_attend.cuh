@@ -602,8 +602,9 @@ __device__ __forceinline__ void write_row(const Params &p, int n, int h, const f
 }
 
 // Without prefixes: what there is to join are the items that were cut, at most one per worker that begins one it does not end.  A
-// CTA per worker, a warp per row.  (Looking at every row and head instead: 111 us for the 358000 of four prompts of 2980 tokens, of
+// few CTAs per worker, a warp per row, two rows a warp.  (Looking at every row and head instead: 111 us for the 358000 of four prompts of 2980 tokens, of
 // which nearly none is cut.)
+constexpr int kCutRows = 16; // of a CTA
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, const Pieces f)
 {
@@ -615,7 +616,7 @@ __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, co
     const int last = f.items[o.item].y;
     if (last <= first || last >= f.n_workers) return; // (a worker that gave up left its items unnoted)
     const int all = last - first + 1, rows = min(f.M, o.n_q * p.R - o.r0);
-    for (int r = warp; r < rows; r += 8) {
+    for (int r = blockIdx.y * kCutRows + warp; r < min(rows, (int)(blockIdx.y + 1) * kCutRows); r += 8) {
         // the item's first piece is the last one of its worker, the others are the first ones of theirs
         const auto at = [&](int i) { return (2ll * (first + i) + (i == 0)) * f.M + r; };
         float top = -INFINITY;
@@ -721,9 +722,8 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         for (int i = 0; i < nh; ++i) {
             const long long row = ((long long)n * p.Hq + h0 + i) * D;
             const float u0 = __shfl_sync(0xffffffffu, w0, i), u1 = __shfl_sync(0xffffffffu, w1, i);
-            Lane<D> x, y;
-            if (u0 > 0.0f) x.load(p.whole[0].o + row);
-            if (u1 > 0.0f) y.load(p.whole[1].o + row);
+            Lane<D> x, y; // (asked for before the weights are known; where a weight is 0 they may hold anything)
+            x.load(p.whole[0].o + row), y.load(p.whole[1].o + row);
             float acc[kPer];
 #pragma unroll
             for (int d = 0; d < kPer; ++d) acc[d] = (u0 > 0.0f ? x.v[d] * u0 : 0.0f) + (u1 > 0.0f ? y.v[d] * u1 : 0.0f);

@@ -96,8 +96,8 @@ size_t cache_bytes(const dart_cache *c) { return (size_t)c->n_pages * c->n_heads
 
 // ---- attention ---------------------------------------------------------------------------------------------------------------
 
-constexpr int kJoinFew = 2048;   // (row, head) pairs up to which eight warps join one
-constexpr int kJoinMany = 16384; // ... and one warp; beyond, a warp joins eight
+// Warps that join a (row, head) pair, by how many pairs there are: sixteen, four, one; beyond kJoinMany a warp joins several
+constexpr int kJoinOne = 256, kJoinFew = 4096, kJoinMany = 16384;
 
 enum Form { NARROW, WIDE, PAIR };
 
@@ -302,11 +302,12 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     }
     j.p = p;
     const long long pairs = (long long)a->n_rows * a->n_q_heads;
-    const int heads = pairs <= kJoinMany ? 1 : 8;
+    const int heads = pairs <= kJoinMany ? 1 : 4;
     const long long warps = a->n_rows * ((a->n_q_heads + heads - 1ll) / heads);
-    const cudaError_t e = pairs <= kJoinFew       ? launch_next(attend_join_rows_kernel<T, D, 8>, dim3((unsigned)pairs), 256, 0, st, j, 1)
+    const cudaError_t e = pairs <= kJoinOne    ? launch_next(attend_join_rows_kernel<T, D, 16>, dim3((unsigned)pairs), 512, 0, st, j, 1)
+                          : pairs <= kJoinFew  ? launch_next(attend_join_rows_kernel<T, D, 4>, dim3((unsigned)pairs), 128, 0, st, j, 1)
                           : a->n_groups > 0 ? launch_next(attend_join_rows_kernel<T, D, 1>, dim3((unsigned)((warps + 3) / 4)), 128, 0, st, j, heads)
-                                            : launch_next(attend_join_cut_kernel<T, D>, dim3((unsigned)j.from[1].n_workers), 256, 0, st, p, j.from[1]);
+                                            : launch_next(attend_join_cut_kernel<T, D>, dim3((unsigned)j.from[1].n_workers, (unsigned)((j.from[1].M + kCutRows - 1) / kCutRows)), 256, 0, st, p, j.from[1]);
     const cudaError_t e2 = cudaGetLastError();
     return e == cudaSuccess && e2 == cudaSuccess ? DART_OK : DART_ERR_CUDA;
 }
