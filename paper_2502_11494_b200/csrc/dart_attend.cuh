@@ -67,7 +67,7 @@ struct Params {
     float scale_log2;               // scale / ln 2: exponentials are powers of two
     int32_t *status;                // 4 words
     int n_prefix, n_own;            // segments of this launch: prefixes first
-    int n_workers, max_items;
+    int n_workers, max_items, least; // least: the most that a share's least size may be
     Pieces pieces;
     Whole whole[2];                 // [0] prefixes, [1] own tokens
 };
@@ -143,7 +143,7 @@ template <int kWorkers>
 struct PlanShared {
     Start start[kWorkers];
     long long room[32], items[32];
-    int each, more; // shares of the line: every worker's `each`, the first `more` of them one more
+    int each, more, all; // shares of the line: every worker's `each`, the first `more` of them one more, as far as it goes
 };
 
 // Every CTA finds where its workers begin.  Block-wide; ends with a barrier.  (The line's length is counted in 32 bits: 2^31 tiles would
@@ -175,16 +175,20 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
         i_all += sh.items[w], r_all += sh.room[w];
     }
     const bool ok = i_all <= p.max_items && r_all < 0x7fffffffll;
-    const int each = ok ? (int)((unsigned)r_all / (unsigned)p.n_workers) : 0, more = ok ? (int)r_all - each * p.n_workers : 0;
+    int each = ok ? (int)((unsigned)r_all / (unsigned)p.n_workers) : 0, more = ok ? (int)r_all - each * p.n_workers : 0;
+    // Long items in small shares are slower to join than to read (narrow form, us a call, shares of 1, 2, 4 tiles at least: one sequence of 300
+    // tokens 12.8, 14.1, 18.0; of 6000 23.2, 19.8, 20.6; of 24000 34.5, 34.5, 31.6): a tile for each 64 of an item, up to p.least.
+    const int least = ok && p.least > 1 ? min(p.least, (int)((unsigned)r_all / ((unsigned)max(i_all, 1ll) * 64u + 1u))) : 1;
+    if (each < max(least, 1)) each = max(least, 1), more = 0;
     if (tid == 0) {
-        sh.each = each, sh.more = more;
+        sh.each = each, sh.more = more, sh.all = ok ? (int)r_all : 0;
         if (!ok && p.status) *p.status = kErrCheck;
     }
     if (ok && room > 0) {
         const int begin = (int)(r_sum - room), end = (int)r_sum; // the thread's part of the line
 #pragma unroll 1
         for (int i = 0; i < kWorkers; ++i) {
-            const int w = blockIdx.x * kWorkers + i, at = each * w + min(w, more);
+            const int w = blockIdx.x * kWorkers + i, at = w > 0x3fffffff / max(each, 1) ? 0x7fffffff : each * w + min(w, more);
             if (at < begin || at >= end) continue;
             int base = (int)(i_sum - items), first = begin, s = s0;
             for (;; ++s) { // (with one segment a thread it is at hand)
@@ -233,7 +237,8 @@ struct Walk {
     __device__ __forceinline__ void begin(const Params &p, const PlanShared<kWorkers> &sh, int local)
     {
         worker = blockIdx.x * kWorkers + local;
-        left = sh.each + (worker < sh.more);
+        const int at = worker > 0x3fffffff / max(sh.each, 1) ? sh.all : sh.each * worker + min(worker, sh.more);
+        left = max(0, min(sh.each + (worker < sh.more), sh.all - at));
         done = left == 0;
         if (done) return;
         const Start &st = sh.start[local];
@@ -323,7 +328,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? (m
 // what the joining launch merges anyway).  Keys and values of 32 tokens take turns in the ring; with three places of 8 KB and eight
 // warps 128 KB are on their way per SM, which covers the latency of HBM at its full rate.  Tokens behind the end of a sequence
 // are filled with zeros in shared memory, whatever their page holds: 0 * NaN would be NaN.
-constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8, kNarrowCost = 1;
+constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8, kNarrowCost = 1, kNarrowLeast = 4;
 constexpr int kNarrowRing = 24576; // bytes of a warp's ring
 
 template <typename T>

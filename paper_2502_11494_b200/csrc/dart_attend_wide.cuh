@@ -29,7 +29,7 @@ using sweep::smem_u32;
 using sweep::umma_commit;
 using sweep::umma_desc;
 
-constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384, kWideCost = 2;
+constexpr int kWideRows = 128, kWideTile = 128, kWideThreads = 384, kWideCost = 3;
 constexpr int kPieces = 4;                      // that may wait for the softmax threads
 constexpr int kHalf = 16384;                    // bytes: 128 tokens (or rows) x 64 columns
 constexpr int kWideSmem = 14 * kHalf + 1024;    // queries, the rings, 4 KB a softmax warp; the base is aligned to 1 KB

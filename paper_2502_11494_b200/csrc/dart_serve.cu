@@ -113,7 +113,8 @@ struct Layout {
     size_t whole_o[2], whole_ml[2], status, bytes;
 };
 
-// Rows of a tile by how many rows a segment has on average (the host knows the sizes, not the lengths).
+// Rows of a tile by how many rows a segment has on average (the host knows the sizes, not the lengths).  64 sequences of 300 to 600 tokens,
+// 8 KV heads, in us: 8 rows each narrow 40, wide 53; 16 rows 36, 50; 32 rows 50, 52; 64 rows 77, 55; 128 rows wide 62, pairs 67; 192 rows 90, 79.
 // A wide tile holds whole tokens, so that a copy can fetch its queries.
 Form form_of(long long rows, long long segments, long long R)
 {
@@ -140,7 +141,11 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     using namespace dart::attend;
     Layout L = {};
     const long long R = a->n_q_heads / c->n_heads;
-    const Form own = form_of(a->n_rows * R, a->n_seq, R), shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups, R) : own;
+    Form own = form_of(a->n_rows * R, a->n_seq, R);
+    const Form shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups, R) : own;
+    // Few sequences go along with their prefixes: one launch instead of two (a prefix of 18432 tokens, 28 query heads, 4 KV heads: 16 sequences 40.6
+    // -> 31.6 us, 32 sequences 41.9 -> 36.9; 64 sequences, more than a worker each, 52.7 and, all in tiles of 256 rows, 55).
+    if (own == NARROW && shared != NARROW && (long long)a->n_seq * c->n_heads <= (shared == WIDE ? 2 : 1) * sms) own = shared;
     L.n = own == shared ? 1 : 2;
     L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = own == shared, L.launch[0].form = shared;
     L.launch[1].own = true, L.launch[1].form = own;
@@ -276,7 +281,7 @@ int launch_attend(const dart_cache *c, const dart_attend_args *a, char *ws, cons
     for (int i = 0; i < L.n; ++i) {
         const Launch &l = L.launch[i];
         p.n_prefix = l.prefix ? a->n_groups : 0, p.n_own = l.own ? a->n_seq : 0;
-        p.n_workers = l.n_workers, p.max_items = l.max_items;
+        p.n_workers = l.n_workers, p.least = l.form == NARROW ? kNarrowLeast : 1, p.max_items = l.max_items;
         p.pieces = Pieces{(int *)(ws + l.item_base), (int2 *)(ws + l.items), (float *)(ws + l.o), (float2 *)(ws + l.ml), (Open *)(ws + l.open), l.M, l.n_workers, divisor(l.M)};
         for (int k = 0; k < 2; ++k)
             if (k ? l.own : l.prefix) j.from[k] = p.pieces, j.seg_off[k] = k ? p.n_prefix : 0, j.n_seg[k] = l.n_seg;
