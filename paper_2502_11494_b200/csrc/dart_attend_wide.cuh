@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         {
             const int ring = kPair ? 0 : warp - 10, k0 = kPair ? warp - 10 : 0, k1 = kPair ? warp - 9 : 2;
             const bool first = k0 == 0;
-            Walk<kWideTile, kWideCost> w;
+            Walk<kWideTile, kWideCost> w{};
             w.begin(p, pl, ring);
             const int box = min(1 << p.page_shift, kWideTile), nowhere = (p.n_pages * p.Hk) << p.page_shift;
             uint32_t tiles = 0, pieces = 0, last = 0; // of the ring so far; the warp's newest copy + 1
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         tmem_wait_st();
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
-                        if (lane == 0 && !(withhold && blockIdx.x == 0 && warp == 0)) mbar_arrive(smem_u32(c == 1 ? &sh.p_half[e] : &sh.p_full[e]));
+                        if (lane == 0 && !(withhold && warp == 0)) mbar_arrive(smem_u32(c == 1 ? &sh.p_half[e] : &sh.p_full[e]));
                     }
                 }
                 l += (l0 + l1) + (l2 + l3);

@@ -342,3 +342,113 @@ def test_wrong_arguments_are_refused():
     assert c.cache.attend(c.q[:0], c.table, c.kv_len, cu_q=none).shape == (0, 4, 128)
     a = dart.dart_attend_args(n_rows=2)
     assert dart.dart_attend(c.cache._c, a, None, 0, ctypes.c_void_p(0)) == dart.DART_ERR_BAD_SHAPE
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hk,D,seqs,groups", [
+    (20, 1, 128, [(1, 700), (1, 31)], []), (128, 1, 64, [(1, 300)], []), (130, 1, 64, [(1, 300)], []), (33, 1, 128, [(9, 200), (1, 3)], [(2, 260)]),
+    (4, 4, 128, [(128, 128), (129, 129), (127, 300)], []), (4, 4, 64, [(255, 255), (256, 256), (257, 500)], []), (14, 2, 128, [(18, 18), (37, 64)], [(1, 127), (1, 129)]),
+    (8, 8, 64, [(200, 200)] * 3, [(3, 1)]), (6, 3, 128, [(90, 0), (70, 35), (65, 64)], [(1, 0), (2, 250)]),
+])
+def test_wide_tiles_at_their_edges(dtype, Hq, Hk, D, seqs, groups):
+    """Rows of one token that do and do not fill a tile of 128, more query heads a KV head than a tile has rows, sequences that end beside a tile's
+    end, engines without rows or without a token to see."""
+    Case(Hq, Hk, D, 16, dtype, seqs, groups=groups, gap=1).check()
+
+
+@pytest.mark.parametrize("q,groups", [(1, True), (40, False), (140, False)])
+def test_a_wait_that_runs_out_is_reported(q, groups):
+    """A hand-over that is withheld on purpose (a barrier that one warp never arrives at): the kernel gives up after 20 ms, frees its tensor memory
+    and says which wait it was; the next call is served."""
+    c = Case(8, 2, 128, 16, "bf16", [(q, 400)] * (20 if groups else 2), groups=[(20, 900)] if groups else [])
+    want = c.check()[0].clone()
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    out = torch.zeros((c.n, 8, 128), dtype=torch.bfloat16, device="cuda")
+    pt, pl, cg = c.prefix or (None, None, None)
+    a = dart.dart_attend_args(p(c.q), p(out), None, c.q.stride(0), out.stride(0), c.n, 8, len(c.seqs), len(c.groups), p(c.cu_q), p(c.table), p(c.kv_len), p(cg), p(pt), p(pl),
+                              c.table.stride(0), pt.stride(0) if groups else 0, 128 ** -0.5, 20000, p(status), 1)
+    need = dart.dart_attend_workspace(c.cache._c, a)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    assert dart.dart_attend(c.cache._c, a, p(ws), need, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == dart.DART_OK
+    torch.cuda.synchronize()
+    got = status.tolist()
+    assert got[0] == dart.DART_ERR_TIMEOUT and 110 <= got[1] <= 125, got
+    again = c.check()[0]
+    mine = slice(c.cu[0], c.cu[-1])
+    assert torch.equal(again[mine], want[mine])
+
+
+def test_threads_call_at_once():
+    import threading
+
+    cases = [Case(8, 2, 128, 16, "bf16", [(n, 300 + 17 * i)] * 6, groups=[(6, 500)], seed=i) for i, n in enumerate((1, 40, 1, 40))]
+    want = [c.check(with_lse=False)[0].clone() for c in cases]
+    bad = []
+
+    def work(c, w):
+        s = torch.cuda.Stream()
+        for _ in range(20):
+            out = c.cache.attend(c.q, c.table, c.kv_len, cu_q=c.cu_q, prefix=c.prefix, stream=s)
+            s.synchronize()
+            if not torch.equal(out, w):
+                bad.append(c)
+
+    threads = [threading.Thread(target=work, args=x) for x in zip(cases, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+def test_from_projection_to_answer():
+    """The operators as they are used together: keys normalised and rotated, scored and reduced; the kept rows into pages; questions about each image
+    behind its shared, shortened prompt; then a decoding step."""
+    B, S, Hq, Hk, D, P, Kp, vo, nv, Q = 2, 260, 8, 2, 64, 4, 50, 12, 220, 3
+    g = _gen(77)
+    rows = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    inv = (1.0 / 10000.0 ** (torch.arange(0, D, 2, dtype=torch.float64) / D)).float().cuda()
+    rope, w = dart.Rope(inv), (1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(torch.bfloat16)
+    k0, v0, hidden = rows(B * S, Hk, D), rows(B * S, Hk, D), rows(B, S, Hk * D)
+    pos = torch.arange(S, device="cuda").repeat(B)
+    _, keys = dart.norm_rope(None, k0, pos=pos, rope=rope, k_weight=w)
+    ctx = dart.Dart(B, S, Hk * D, P, Kp)
+    out_hidden, idx, out_pos = ctx.reduce(hidden, keys.view(B, S, Hk * D), vo, nv, P, Kp)
+    S_out = S - nv + Kp
+    n_seq, per = B * Q, (S_out + 15) // 16
+    kc, vc = rows(B * per + n_seq * 2, Hk, 16, D), rows(B * per + n_seq * 2, Hk, 16, D)
+    ids = torch.randperm(kc.shape[0], generator=g, device="cuda").to(torch.int32)
+    ptable, table = ids[:B * per].view(B, per), ids[B * per:].view(n_seq, 2)
+    cache = dart.PagedCache(kc, vc)
+    cache.append(k0, v0, ptable, idx=idx, S=S, pos=out_pos, rope=rope, k_weight=w)  # from the rows before the rotation: the same keys
+    prefix = (ptable, torch.full((B,), S_out, dtype=torch.int32, device="cuda"), torch.arange(0, n_seq + 1, Q, dtype=torch.int32, device="cuda"))
+    have, own_k, own_v = 0, [[] for _ in range(n_seq)], [[] for _ in range(n_seq)]
+    for n in (13, 1, 1):  # the questions, then two tokens of the answers
+        q1, k1, v1 = rows(n_seq * n, Hq, D), rows(n_seq * n, Hk, D), rows(n_seq * n, Hk, D)
+        at = (S + have + torch.arange(n, device="cuda")).repeat(n_seq)
+        q2, k2 = dart.norm_rope(q1, k1, pos=at, rope=rope, q_weight=w, k_weight=w)
+        start = torch.full((n_seq,), have, dtype=torch.int32, device="cuda")
+        cache.append(k1, v1, table, start=start, pos=at, rope=rope, k_weight=w)
+        have += n
+        cu = torch.arange(0, n_seq * n + 1, n, dtype=torch.int32, device="cuda")
+        out = cache.attend(q2, table, start + n, cu_q=cu, prefix=prefix)
+        assert cache.status() == dart.DART_OK and ctx.status() == dart.DART_OK
+        for s in range(n_seq):
+            own_k[s].append(k2[s * n:(s + 1) * n]), own_v[s].append(v1[s * n:(s + 1) * n])
+            b = s // Q
+            kept = idx[b].long()
+            K = torch.cat([keys.view(B, S, Hk, D)[b, kept]] + own_k[s]).double().repeat_interleave(Hq // Hk, 1)
+            V = torch.cat([v0.view(B, S, Hk, D)[b, kept]] + own_v[s]).double().repeat_interleave(Hq // Hk, 1)
+            x = q2[s * n:(s + 1) * n].double()
+            logits = torch.einsum("nhd,lhd->hnl", x, K) / D ** 0.5
+            hidden_from = S_out + have - n + torch.arange(n, device="cuda") + 1
+            logits = logits.masked_fill(torch.arange(K.shape[0], device="cuda")[None, :] >= hidden_from[:, None], -math.inf)
+            p = logits.softmax(-1)
+            want, size = torch.einsum("hnl,lhd->nhd", p, V), torch.einsum("hnl,lhd->nhd", p, V.abs())
+            # output and weights rounded to bf16: half a step each; the scores' sums of 64 products in fp32: 68 * 2^-23 of |q||k| / 8 <= 20
+            bound = 2.0**-8 * want.abs() + (2.0**-8 + 2 * 68 * 2.0**-23 * 20 + 1e-4) * size * (1 + 2.0**-8)
+            off = (out[s * n:(s + 1) * n].double() - want).abs()
+            assert bool((off <= bound).all()) and float(x.norm(dim=-1).max() * K.norm(dim=-1).max()) / 8 < 20
+    assert torch.equal(out_hidden, torch.gather(hidden, 1, idx.long()[..., None].expand(-1, -1, Hk * D)))
+    ctx.close()

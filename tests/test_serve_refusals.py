@@ -97,3 +97,40 @@ def test_append_takes_slots_as_positions_on_one_axis_only(dart):
 def test_struct_layouts(dart):
     assert ctypes.sizeof(dart.dart_rope) == 32 and dart.dart_rope.rot_dim.offset == 8 and dart.dart_rope.section.offset == 20
     assert ctypes.sizeof(dart.dart_cache) == 40 and dart.dart_cache.n_pages.offset == 16
+
+
+def _attend(dart, cache=None, ws=1 << 30, ws_bytes=1 << 40, **kw):
+    c = dict(k=C, v=D_, n_pages=16, n_heads=2, page_size=16, head_dim=128, dtype=0, device=0)
+    c.update(cache or {})
+    a = dict(q=A, out=B, lse=None, q_stride=1024, out_stride=1024, n_rows=4, n_q_heads=8, n_seq=4, n_groups=0, cu_q=None, table=A, kv_len=A, cu_group=None,
+             prefix_table=None, prefix_len=None, table_stride=4, prefix_stride=0, scale=0.1, wait_limit=0, status=None, test_withhold=0)
+    a.update(kw)
+    cache, args = dart.dart_cache(*c.values()), dart.dart_attend_args(*a.values())
+    return dart.dart_attend(cache, args, ws, ws_bytes, None), dart.dart_attend_workspace(cache, args)
+
+
+GROUPS = dict(n_groups=2, cu_group=A, prefix_table=A, prefix_len=A, prefix_stride=4)
+
+
+@pytest.mark.parametrize("cache,kw,code", [
+    (dict(v=None), {}, -1), (dict(head_dim=96), {}, -9), (dict(head_dim=256), {}, -9), (dict(page_size=8), {}, -9), (dict(page_size=48), {}, -9),
+    (dict(page_size=2048), {}, -9), (dict(dtype=3), {}, -9), (dict(n_pages=0), {}, -2), (dict(n_pages=1 << 27), {}, -2), (dict(v=D_ + 8), {}, -3),
+    ({}, dict(n_rows=-1), -2), ({}, dict(n_seq=0), -2), ({}, dict(n_groups=-1), -2), ({}, dict(n_q_heads=0), -2), ({}, dict(n_q_heads=7), -2), ({}, dict(table_stride=0), -2),
+    ({}, dict(scale=0.0), -2), ({}, dict(scale=-1.0), -2), ({}, dict(scale=float("nan")), -2), ({}, dict(scale=float("inf")), -2), ({}, dict(n_rows=5), -2),
+    ({}, dict(wait_limit=-1), -2), ({}, dict(q_stride=1016), -2), ({}, dict(out_stride=1020), -2), ({}, dict(n_rows=1 << 28, cu_q=A), -2), ({}, dict(table_stride=1 << 28), -2),
+    ({}, dict(GROUPS, prefix_stride=0), -2), ({}, dict(GROUPS, prefix_len=None), -1), ({}, dict(GROUPS, cu_group=None), -1),
+    ({}, dict(q=None), -1), ({}, dict(out=None), -1), ({}, dict(table=None), -1), ({}, dict(kv_len=None), -1), ({}, dict(q=A + 8), -3), ({}, dict(out=B + 8), -3),
+    ({}, dict(kv_len=A + 2), -3), ({}, dict(status=A + 3), -3), ({}, dict(lse=A + 2), -3),
+    ({}, dict(out=A), -4), ({}, dict(out=C), -4), ({}, dict(out=D_ + 16), -4), ({}, dict(lse=B), -4), ({}, dict(lse=A + 1024), -4), ({}, dict(lse=C), -4),
+])
+def test_attend_refuses(dart, cache, kw, code):
+    assert _attend(dart, cache, **kw) == (code, 0)
+
+
+def test_attend_wants_its_workspace(dart):
+    rc, need = _attend(dart, ws_bytes=255)
+    assert rc == dart.DART_ERR_NOMEM and need > 255 and need % 256 == 0
+    assert _attend(dart, ws=None)[0] == dart.DART_ERR_NULL and _attend(dart, ws=(1 << 30) + 128)[0] == dart.DART_ERR_ALIGN
+    assert _attend(dart, n_rows=0, cu_q=A) == (dart.DART_OK, 0) and _attend(dart, **GROUPS)[1] > need
+    assert dart.dart_attend(None, None, None, 0, None) == dart.DART_ERR_NULL
+    assert ctypes.sizeof(dart.dart_attend_args) == 136 and dart.dart_attend_args.scale.offset == 112 and dart.dart_attend_args.status.offset == 120
