@@ -46,7 +46,7 @@ def parse():
     ap.add_argument("--lag", type=int, default=0, help="fused path: extra tasks between a row's two sweeps")
     ap.add_argument("--retention", type=int, default=0, help="0 auto, 1 one kernel, 2 sorted lists + walks, 3 bands + turns, 4 bands and turns in one launch")
     ap.add_argument("--variants", action="store_true",
-                    help="also time the variants: one threshold for all pivots, pivots given by the caller, KV-row gather")
+                    help="also time the variants: one threshold for all pivots, pivots given by the caller, KV-row gather, rotated keys, kept rows into a paged cache and attention over it")
     ap.add_argument("--no-e2e", action="store_true")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     return ap.parse_args()
@@ -291,6 +291,46 @@ def time_steps(ctx, dart, torch, w, keys, hidden, outs, steps, warmup, opts, dis
     return ms, per, launches, prof
 
 
+def serve_variants(dart, torch, w, keys, hidden, outs, steps, dev, peak):
+    """What follows a reduction in a serving engine, in heads of 128: the layer's keys normalised and rotated, the kept rows of keys and
+    values put into the pages of a cache by the reduction's own index list, and eight single-token queries per sample over its shortened prompt."""
+    H, page, each = w.d // 128, 64, 8
+    rope = dart.Rope((1.0 / 10000.0 ** (torch.arange(0, 128, 2, dtype=torch.float64) / 128)).float().to(dev))
+    rows = lambda t: t.view(w.B * w.S, H, 128)  # noqa: E731
+    per = (w.S_out + page - 1) // page
+    kc, vc = (torch.zeros((w.B * per + w.B * each, H, page, 128), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    ids = torch.randperm(kc.shape[0], device=dev).to(torch.int32)
+    prompt, own = ids[:w.B * per].view(w.B, per), ids[w.B * per:].view(w.B * each, 1)
+    cache = dart.PagedCache(kc, vc)
+    pos = torch.arange(w.S, device=dev).repeat(w.B)
+    weight = torch.ones(128, dtype=torch.bfloat16, device=dev)
+    turned = torch.empty_like(keys)
+    prefix = (prompt, torch.full((w.B,), w.S_out, dtype=torch.int32, device=dev), torch.arange(0, w.B * each + 1, each, dtype=torch.int32, device=dev))
+    q = torch.randn((w.B * each, H, 128), device=dev).to(torch.bfloat16)
+    out, have = torch.empty_like(q), torch.full((w.B * each,), 1, dtype=torch.int32, device=dev)
+
+    def timed(call):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        for k in range(2 + steps):
+            if k == 2:
+                e0.record()
+            call()
+        e1.record()
+        torch.cuda.synchronize()
+        return e0.elapsed_time(e1) / steps
+
+    found = {}
+    for name, call, n_bytes in (
+            ("norm_rope_keys", lambda: dart.norm_rope(None, rows(keys), pos=pos, rope=rope, k_weight=weight, out=(None, rows(turned))), 4 * keys.numel()),
+            ("kept_rows_to_pages", lambda: cache.append(rows(keys), rows(hidden), prompt, idx=outs[1], S=w.S, pos=outs[2], rope=rope), 8 * w.B * w.S_out * w.d),
+            ("attend_shared_prompt", lambda: cache.attend(q, own, have, prefix=prefix, out=out), 4 * w.B * (w.S_out + each) * w.d + 4 * q.numel())):
+        ms = timed(call)
+        found[name] = {"ms_per_call": ms, "achieved_GBps": n_bytes / (ms * 1e-3) / 1e9, "frac_of_measured_copy": n_bytes / (ms * 1e-3) / 1e9 / peak}
+    if cache.status() != 0:
+        raise RuntimeError("the cache's status word reports an error")
+    return found
+
+
 def oracle_leg(w, keys, hidden, ref_idx, budget_s):
     """The CPU baseline: the oracle as it stands, single-threaded on one core (the stated baseline) and the same
     single-threaded code over samples on all host cores (context).  The samples it computes are also compared with the
@@ -478,6 +518,8 @@ def main():
         gbs = 2 * (2 * w.d * w.S_out) * B / (ms_k * 1e-3) / 1e9
         variants["kv_row_gather"] = {"ms_per_launch": ms_k, "achieved_GBps": gbs, "frac_of_measured_copy": gbs / peak}
         del packed, piv
+        if w.d % 128 == 0:
+            variants.update(serve_variants(dart, torch, w, keys, hidden, outs, n_v, dev, peak))
 
     e2e = None
     if not args.no_e2e:

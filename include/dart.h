@@ -451,7 +451,7 @@ typedef struct {
     int32_t wait_limit;           /* 0: default (2 s); > 0: time limit in microseconds of every bounded device-side wait */
     int32_t *status;              /* [4] device, or NULL.  status[0] becomes DART_ERR_CHECK where a page of a visible token is outside the
                                      cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
-                                     do not ascend (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
+                                     that do not ascend name more rows than there are (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
                                      status[1..3] say which wait, item and CTA */
     int32_t test_withhold;        /* testing only: nonzero withholds one hand-over inside the kernel that waits */
 } dart_attend_args;

@@ -1,8 +1,8 @@
 // Attention over the paged cache for many rows: tiles of 128 rows on the tensor cores (see dart_attend.cuh for the work's division
 // and for how pieces are joined).
 //
-// A CTA has two ENGINES of a 128-row tile each: four softmax warps with a thread per
-// row, 256 columns of tensor memory; one thread issues tcgen05.mma for both.  For each KV tile of 128 tokens an engine does
+// A CTA has two ENGINES of a 128-row tile each: four softmax warps with a thread per row, 256 columns of tensor memory.  For each KV
+// tile of 128 tokens an engine does
 //   S = Q K^T   (Q and K in shared memory, 128-byte swizzle, S in tensor memory),
 //   P = 2^(S scale - m), in the cache's type, written over S,
 //   O += P V    (P from tensor memory, V as it lies in the cache: tokens along the product's inner dimension),
@@ -10,9 +10,16 @@
 // exponential unit a tile, the two that bound it.  O stays in tensor memory over a whole piece; it is only scaled when a
 // row's maximum has grown by more than 2^8 since it was last (fp32 sums and 16-bit weights lose nothing by a common factor).
 //   kPair false: the engines are two workers with a ring of tiles each (a place: keys or values of 128 tokens).
-//   kPair true:  they are one worker, 256 rows: both multiply with the same tiles.  Half the traffic from L2.
+//   kPair true:  they are one worker, two row tiles, whose products one warp issues in turn: both multiply with the same KV tiles.  Half the
+//                traffic from L2.
 // Rows behind a sequence's end come from its last page as they are; their scores are left out by selection, and the values among
 // the last 16 tokens of a product are set to zero in shared memory (0 * NaN would be NaN).
+// What bounds it (128 columns, 256 rows, cycles of one KV tile): 2048 of the tensor pipe for both engines, 3800 measured: an engine's softmax takes
+// 2000 from its scores to its weights (load 100, maximum 440, exponentials 1500), and what hands over between the warps 1300 more; the
+// engines overlap, but not fully.  A piece's end takes some 10000 (its rows by way of shared memory, the next piece's queries and first scores).
+// Tried and taken back: three of eight exponentials as polynomials on the FMA pipe (2600 instead of 1390), two threads a row (eight warps an
+// engine: their meeting costs 1000), a warp per engine for the products (both engines fall into step, at the exponentials together and at the
+// products together: 4600), the same with a turn for the exponentials (4150).
 // Every wait is bounded in time; a kernel that gives up says so in the status word, waits for its own copies and products, frees
 // the tensor memory and returns.
 #pragma once

@@ -347,6 +347,15 @@ def _code(dtype):
     return _CODES[dtype]
 
 
+def _on(stream, device, index):
+    """The stream of a call as a number: the caller's, or the device's current one."""
+    if stream is None:
+        return _raw_stream(index)
+    if stream.device != device:
+        raise ValueError("the stream must be of the rows' device")
+    return stream.cuda_stream
+
+
 def _head_rows(t, name, dtype, device, n_rows, D):
     """Rows [n_rows, heads, D] with the heads of a row side by side -> (address, values from row to row, heads)."""
     shape, stride = t.shape, t.stride()
@@ -429,7 +438,7 @@ def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6,
         turn = rope.at(pos, n, dev)
     rc = lib().dart_norm_rope(qa[0], qa[1], qa[2], ka[0], ka[1], ka[2], n, D, code, _vector(q_weight, "q_weight", D, dtype, dev),
                               _vector(k_weight, "k_weight", D, dtype, dev), eps, turn[0], turn[1], turn[2], qo[0], qo[1], ko[0], ko[1], index,
-                              stream.cuda_stream if stream is not None else _raw_stream(index))
+                              _on(stream, dev, index))
     if rc != DART_OK:
         raise DartError(rc, "dart_norm_rope")
     return out
@@ -489,7 +498,7 @@ class PagedCache:
         rc = lib().dart_cache_append(self._c, ka[0], ka[1], va[0], va[1], n_seq, n, self._ints(cu_rows, "cu_rows", n_seq + 1), self._ints(idx, "idx"),
                                      S, tp, ts, self._ints(start, "start", n_seq), _vector(k_weight, "k_weight", D, dtype, dev), eps,
                                      turn[0], turn[1], turn[2], self._status_at,
-                                     stream.cuda_stream if stream is not None else _raw_stream(self._index))
+                                     _on(stream, dev, self._index))
         if rc != DART_OK:
             raise DartError(rc, "dart_cache_append")
 
@@ -499,7 +508,8 @@ class PagedCache:
         lengths [groups], cu_group [groups + 1]) the tokens that a group of sequences shares.  ``cu_q`` [sequences + 1]: ragged
         numbers of rows (None: one row per sequence).  ``scale``: None for 1 / sqrt(D).  Returns ``out`` (made if None); ``lse``, a
         fp32 tensor [N, Hq], is filled if given."""
-        if stream is not None: # (what is made below is made for that stream)
+        if stream is not None:  # (what is made below is made for that stream)
+            _on(stream, self.device, self._index)
             with self._torch.cuda.stream(stream):
                 return self.attend(q, table, kv_len, cu_q, prefix, scale, out, lse, wait_limit)
         dev, dtype, D = self.device, self.dtype, self.head_dim
