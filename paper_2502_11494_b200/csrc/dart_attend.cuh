@@ -329,6 +329,8 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? (m
 // what the joining launch merges anyway).  Keys and values of 32 tokens take turns in the ring; with three places of 8 KB and eight
 // warps 128 KB are on their way per SM, which covers the latency of HBM at its full rate.  Tokens behind the end of a sequence
 // are filled with zeros in shared memory, whatever their page holds: 0 * NaN would be NaN.
+// Measured: 64 sequences of 164 to 676 tokens, 32 heads of 128, 91 us = 5.5 TB/s; two of 99000 and 131072 tokens, 4 KV heads, 88 us = 5.8 TB/s (copy
+// rate 6.55).  Room of 0, 2, 4 tiles an item: 1, 1, 3 % slower; L2 prefetch hints on the copies: no difference.
 constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8, kNarrowCost = 1, kNarrowLeast = 4;
 constexpr int kNarrowRing = 24576; // bytes of a warp's ring
 
