@@ -453,7 +453,8 @@ typedef struct {
                                      cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
                                      that do not ascend name more rows than there are (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
                                      status[1..3] say which wait, item and CTA */
-    int32_t test_withhold;        /* testing only: nonzero withholds one hand-over inside the kernel that waits */
+    int32_t test_withhold;        /* testing only: 1 withholds one hand-over inside the kernel that waits, 2 lets the wait for a tile's queries
+                                     give up at once, while their copy may still be under way */
 } dart_attend_args;
 
 /*

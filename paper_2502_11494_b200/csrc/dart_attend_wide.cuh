@@ -64,6 +64,7 @@ struct WideShared {
     unsigned long long full[2][kMaxPlaces], empty[2][kMaxPlaces];
     unsigned long long s_full[2], p_half[2], p_full[2], o_full[2], q_full[2], drain[2];
     uint32_t note[2][kMaxPlaces]; // what a place holds (kNote*), for the thread that issues the products
+    uint32_t asked[2];            // query copies that an engine has begun so far
     uint32_t tmem;
     int abort;
     PlanShared<2> plan;
@@ -224,6 +225,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             mbar_init(smem_u32(&sh.o_full[e]), 1);
             mbar_init(smem_u32(&sh.drain[e]), 1);
             mbar_init(smem_u32(&sh.q_full[e]), 1);
+            sh.asked[e] = 0;
         }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -358,6 +360,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             };
             uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};
             const auto queries = [&](int e) { // a piece's queries are there
+                if (withhold == 2) {
+                    if (issues) ctl.ctl.give_up(kWaitQueries, -1);
+                    __syncwarp();
+                    return false;
+                }
                 return wait(smem_u32(&sh.q_full[e]), n_q[e]++ & 1u, kWaitQueries);
             };
             const auto scores = [&](int e, int at) {
@@ -494,6 +501,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 // rows behind the segment's last are whatever comes next: nobody reads what comes of them
                 const uint32_t bar = smem_u32(&sh.q_full[e]);
                 mbar_arrive_expect_tx(bar, (uint32_t)(rows * D * 2));
+                ++sh.asked[e];
 #pragma unroll
                 for (int hh = 0; hh < kHalves; ++hh) tma_queries(q_at(e) + hh * kHalf, &tm_q, hh * 64, w->hk, n0, bar);
             }
@@ -564,7 +572,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         tmem_wait_st();
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
-                        if (lane == 0 && !(withhold && warp == 0)) mbar_arrive(smem_u32(c == 1 ? &sh.p_half[e] : &sh.p_full[e]));
+                        if (lane == 0 && !(withhold == 1 && warp == 0)) mbar_arrive(smem_u32(c == 1 ? &sh.p_half[e] : &sh.p_full[e]));
                     }
                 }
                 l += (l0 + l1) + (l2 + l3);
@@ -644,6 +652,9 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 }
             }
         }
+        // a CTA that gives up does not end before the engine's query copy has landed either: the products need not have come to wait for it
+        if (!ok && (warp & 3) == 0 && lane == 0 && sh.asked[e] > 0) ctl.wait_landed(smem_u32(&sh.q_full[e]), (sh.asked[e] - 1u) & 1u);
+        __syncwarp();
     }
     // ---------------------------------------------------------------------- end
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

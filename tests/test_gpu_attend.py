@@ -379,6 +379,31 @@ def test_a_wait_that_runs_out_is_reported(q, groups):
     assert torch.equal(again[mine], want[mine])
 
 
+@pytest.mark.parametrize("q,groups", [(1, True), (40, False), (140, False)])
+def test_a_kernel_that_gives_up_waits_for_its_queries(q, groups):
+    """The products give up at the first tile whose queries they would wait for, so that the copy may still be under way when the others learn
+    of it: the block has to wait for it before it ends.  The wait is named, and calls that follow at once, on the same SMs, are served."""
+    c = Case(8, 2, 128, 16, "bf16", [(q, 400)] * (20 if groups else 2), groups=[(20, 900)] if groups else [])
+    want = c.check()[0].clone()
+    p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    out = torch.zeros((c.n, 8, 128), dtype=torch.bfloat16, device="cuda")
+    pt, pl, cg = c.prefix or (None, None, None)
+    status = torch.zeros((4, 4), dtype=torch.int32, device="cuda")
+    again = []
+    for one in status:
+        a = dart.dart_attend_args(p(c.q), p(out), None, c.q.stride(0), out.stride(0), c.n, 8, len(c.seqs), len(c.groups), p(c.cu_q), p(c.table), p(c.kv_len), p(cg), p(pt),
+                                  p(pl), c.table.stride(0), pt.stride(0) if groups else 0, 128 ** -0.5, 20000, p(one), 2)
+        need = dart.dart_attend_workspace(c.cache._c, a)
+        ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        assert dart.dart_attend(c.cache._c, a, p(ws), need, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == dart.DART_OK
+        again.append(c.cache.attend(c.q, c.table, c.kv_len, cu_q=c.cu_q, prefix=c.prefix))
+    torch.cuda.synchronize()
+    for got in status.tolist():
+        assert got[0] == dart.DART_ERR_TIMEOUT and got[1] == 113, got  # kWaitQueries
+    mine = slice(c.cu[0], c.cu[-1])
+    assert all(torch.equal(x[mine], want[mine]) for x in again) and c.cache.status() == dart.DART_OK
+
+
 def test_threads_call_at_once():
     import threading
 
