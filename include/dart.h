@@ -451,7 +451,8 @@ typedef struct {
     int32_t wait_limit;           /* 0: default (2 s); > 0: time limit in microseconds of every bounded device-side wait */
     int32_t *status;              /* [4] device, or NULL.  status[0] becomes DART_ERR_CHECK where a page of a visible token is outside the
                                      cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
-                                     that do not ascend name more rows than there are (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
+                                     that do not ascend name more rows than there are, or the work has 2^31 pairs of a tile of rows and a tile of tokens or
+                                     more (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
                                      status[1..3] say which wait, item and CTA */
     int32_t test_withhold;        /* testing only: 1 withholds one hand-over inside the kernel that waits, 2 lets the wait for a tile's queries
                                      give up at once, while their copy may still be under way */
@@ -462,7 +463,8 @@ typedef struct {
  * it; calls that may overlap (other streams, captured graphs) need one each.  The size depends on sizes only, not on
  * lengths; 0 for arguments that dart_attend refuses and for n_rows 0 (which does nothing).
  * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, else UNSUPPORTED; fewer than 2^30 (row, head) pairs and 2^31 cached (head, token)
- * pairs.  Keys and values of visible tokens must be finite; whatever else lies in the pages has no influence.
+ * pairs.  What the lengths ask for is known on the device only: 2^31 pairs of a tile of 16 or 128 rows of a KV head and a tile of 32 or 128 tokens (a prompt
+ * of two million rows and 32 heads) are reported there.  Keys and values of visible tokens must be finite; whatever else lies in the pages has no influence.
  * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED, NOMEM (workspace too small), CUDA.
  */
 size_t dart_attend_workspace(const dart_cache *cache, const dart_attend_args *args);

@@ -18,6 +18,7 @@
 #include <cuda_fp16.h>
 
 #include "dart_common.cuh"
+#include "dart_shares.h"
 
 namespace dart {
 namespace attend {
@@ -144,11 +145,11 @@ template <int kWorkers>
 struct PlanShared {
     Start start[kWorkers];
     long long room[32], items[32];
-    int each, more, all; // shares of the line: every worker's `each`, the first `more` of them one more, as far as it goes
+    Shares share;
 };
 
-// Every CTA finds where its workers begin.  Block-wide; ends with a barrier.  (The line's length is counted in 32 bits: 2^31 tiles would
-// be 300 TB of keys and values to read.)
+// Every CTA finds where its workers begin.  Block-wide; ends with a barrier.  (The line's length is counted in 32 bits, every row
+// tile's KV tiles for themselves: a prompt of 2^21 rows and 32 heads in tiles of 256 x 128 would be 2^31.  Longer ones are reported.)
 template <int kTile, int kCost, int kWorkers>
 __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
 {
@@ -175,21 +176,17 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
         if (w == warp) i_sum += i_all, r_sum += r_all;
         i_all += sh.items[w], r_all += sh.room[w];
     }
-    const bool ok = i_all <= p.max_items && r_all < 0x7fffffffll;
-    int each = ok ? (int)((unsigned)r_all / (unsigned)p.n_workers) : 0, more = ok ? (int)r_all - each * p.n_workers : 0;
-    // Long items in small shares are slower to join than to read (narrow form, us a call, shares of 1, 2, 4 tiles at least: one sequence of 300
-    // tokens 12.8, 14.1, 18.0; of 6000 23.2, 19.8, 20.6; of 24000 34.5, 34.5, 31.6): a tile for each 64 of an item, up to p.least.
-    const int least = ok && p.least > 1 ? min(p.least, (int)((unsigned)r_all / ((unsigned)max(i_all, 1ll) * 64u + 1u))) : 1;
-    if (each < max(least, 1)) each = max(least, 1), more = 0;
+    const bool ok = i_all <= p.max_items && r_all <= kLongestLine;
+    const Shares share = Shares::of(ok ? (int)r_all : 0, i_all, p.n_workers, p.least);
     if (tid == 0) {
-        sh.each = each, sh.more = more, sh.all = ok ? (int)r_all : 0;
+        sh.share = share;
         if (!ok && p.status) *p.status = kErrCheck;
     }
     if (ok && room > 0) {
         const int begin = (int)(r_sum - room), end = (int)r_sum; // the thread's part of the line
 #pragma unroll 1
         for (int i = 0; i < kWorkers; ++i) {
-            const int w = blockIdx.x * kWorkers + i, at = w > 0x3fffffff / max(each, 1) ? 0x7fffffff : each * w + min(w, more);
+            const int w = blockIdx.x * kWorkers + i, at = share.begin(w);
             if (at < begin || at >= end) continue;
             int base = (int)(i_sum - items), first = begin, s = s0;
             for (;; ++s) { // (with one segment a thread it is at hand)
@@ -238,8 +235,7 @@ struct Walk {
     __device__ __forceinline__ void begin(const Params &p, const PlanShared<kWorkers> &sh, int local)
     {
         worker = blockIdx.x * kWorkers + local;
-        const int at = worker > 0x3fffffff / max(sh.each, 1) ? sh.all : sh.each * worker + min(worker, sh.more);
-        left = max(0, min(sh.each + (worker < sh.more), sh.all - at));
+        left = sh.share.size(worker);
         done = left == 0;
         if (done) return;
         const Start &st = sh.start[local];

@@ -404,6 +404,24 @@ def test_a_kernel_that_gives_up_waits_for_its_queries(q, groups):
     assert all(torch.equal(x[mine], want[mine]) for x in again) and c.cache.status() == dart.DART_OK
 
 
+def test_lines_of_more_than_2_30_tiles():
+    """72 sequences of 2^29 tokens each, all of them in one page: 1.2e9 tiles of 32 tokens, of which every worker takes its share.  Queries of
+    zeros: every token weighs the same, values of zeros: the answer is exact, the log-sum tells how many tokens were counted (a thread's
+    sum of ones is exact below 2^24; four of them and the pieces of some 17 workers are added in fp32: 30 roundings of 2^-24, and those of the logarithm)."""
+    n, page, pages = 72, 1024, 1 << 19
+    k, v = torch.randn((2, 2, 1, page, 64), device="cuda").to(torch.bfloat16)
+    v[0].zero_()
+    cache = dart.PagedCache(k, v)
+    table = torch.zeros((n, pages), dtype=torch.int32, device="cuda")
+    kv_len = torch.tensor([pages * page - 37 * i for i in range(n)], dtype=torch.int32, device="cuda")
+    out = torch.full((n, 1, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n, 1), 7.0, device="cuda")
+    cache.attend(torch.zeros_like(out), table, kv_len, out=out, lse=lse)
+    assert cache.status() == dart.DART_OK
+    assert bool((out == 0).all())
+    assert bool(((lse[:, 0].double() - kv_len.double().log()).abs() <= 60 * 2.0**-24 + 21 * 2.0**-22).all())
+
+
 def test_threads_call_at_once():
     import threading
 
