@@ -430,7 +430,9 @@ int dart_cache_append(const dart_cache *cache, const void *k, int64_t k_stride, 
  * cu_group[g + 1] - 1 also share a prefix of prefix_len[g] tokens in the pages of prefix_table[g], all of which all their rows see; its keys and
  * values are read for all of them at once.  (Many questions about one reduced image: the packed prompt is the prefix.)
  *   out = sum_j softmax_j(scale q.k_j) v_j over the visible tokens, head h of the queries with head h / (n_q_heads / n_heads) of the
- *   cache; rows that see nothing: out = 0, lse = -inf.  Rows of no sequence are left as they are.
+ *   cache; rows that see nothing: out = 0, lse = -inf.  Rows of no sequence are left as they are.  A row and head that sees something
+ *   but has no softmax, because its query holds a NaN or an infinity (scores that are NaN, +inf, or all -inf), is NaN, lse too; no other
+ *   row or head changes by it.
  * Scores, softmax sums and outputs are held in fp32; the softmax weights enter the second product in the cache's type.
  */
 typedef struct {
@@ -464,7 +466,8 @@ typedef struct {
  * lengths; 0 for arguments that dart_attend refuses and for n_rows 0 (which does nothing).
  * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, else UNSUPPORTED; fewer than 2^30 (row, head) pairs and 2^31 cached (head, token)
  * pairs.  What the lengths ask for is known on the device only: 2^31 pairs of a tile of 16 or 128 rows of a KV head and a tile of 32 or 128 tokens (a prompt
- * of two million rows and 32 heads) are reported there.  Keys and values of visible tokens must be finite; whatever else lies in the pages has no influence.
+ * of two million rows and 32 heads) are reported there.  Keys and values of visible tokens must be finite, and scores of finite queries below 2^27 in size (fp32 tells
+ * no weights apart long before); whatever else lies in the pages has no influence.
  * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED, NOMEM (workspace too small), CUDA.
  */
 size_t dart_attend_workspace(const dart_cache *cache, const dart_attend_args *args);

@@ -41,8 +41,8 @@ struct Whole {
 };
 
 struct Open {
-    int item, row0, n_q, hk, r0; // item < 0: none; its segment's rows, KV head, first row
-    int pad[3];
+    int item, row0, n_q, hk, r0, len; // item < 0: none; its segment's rows and tokens, KV head, first row
+    int pad[2];
 };
 
 // What one launch leaves for the joining one.
@@ -292,7 +292,7 @@ __device__ __forceinline__ void no_open_item(const Params &p, int worker) { p.pi
 template <typename W>
 __device__ __forceinline__ void open_item(const Params &p, const W &w)
 {
-    p.pieces.open[w.worker] = Open{w.item(), w.g.row0, w.g.n_q, w.hk, w.mb * p.pieces.M, {0, 0, 0}};
+    p.pieces.open[w.worker] = Open{w.item(), w.g.row0, w.g.n_q, w.hk, w.mb * p.pieces.M, w.g.len, {0, 0}};
 }
 
 // ---- types --------------------------------------------------------------------------------------------------------------
@@ -316,8 +316,13 @@ __device__ __forceinline__ float exp2_approx(float x) // 2^x, within 2 ulp; 2^-i
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// A row's sum of exponentials is at least 1 where its scores are numbers (the largest weight is not below 1), NaN where one is NaN or
+// +inf, and 0 where it sees nothing - or nothing but scores of -inf, of which there is no softmax either: that becomes NaN at the row's end.
+__device__ __forceinline__ float settled(float l, bool sees_any) { return l == 0.0f && sees_any ? NAN : l; }
+// what the sums are multiplied with; rows that see nothing are zeros
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 // log of the sum of exponentials, natural; -inf for rows that see nothing
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
 // Tiles of 16 rows: bound by the cache's bytes, not by products, so that mma.sync (16 x 8 x 16) is enough.  Every WARP is a worker
@@ -545,7 +550,8 @@ __global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(con
             const int r = i ? r1 : r0;
             if (r >= rows) continue;
             if (w.is_whole() && p.n_groups == 0) {
-                const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
+                l[i] = settled(l[i], lim[i] > 0);
+                const float inv = inverse(l[i]);
                 uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + row_n[i] * p.out_stride + (long long)row_h[i] * (D * 2)) + (c0 >> 1);
 #pragma unroll
                 for (int d = 0; d < kN; ++d) dst[d * 4] = pack2<T>(o[d][2 * i] * inv, o[d][2 * i + 1] * inv);
@@ -598,7 +604,7 @@ template <typename T, int D>
 __device__ __forceinline__ void write_row(const Params &p, int n, int h, const float *acc, float top, float sum)
 {
     const int lane = threadIdx.x & 31;
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float inv = inverse(sum);
     uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + (long long)n * p.out_stride + (long long)h * (D * 2)) + lane * (D / 64);
 #pragma unroll
     for (int d = 0; d < D / 64; ++d) dst[d] = pack2<T>(acc[2 * d] * inv, acc[2 * d + 1] * inv);
@@ -626,7 +632,7 @@ __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, co
         float top = -INFINITY;
         for (int i = lane; i < all; i += 32) {
             const float2 v = f.ml[at(i)];
-            if (v.y > 0.0f) top = fmaxf(top, v.x);
+            if (v.y != 0.0f) top = fmaxf(top, v.x);
         }
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
@@ -636,14 +642,14 @@ __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, co
             const float2 v = f.ml[at(i)];
             Lane<D> x;
             x.load(f.o + at(i) * D);
-            if (!(v.y > 0.0f)) continue;
+            if (v.y == 0.0f) continue;
             const float wgt = exp2_approx(v.x - top);
             sum += v.y * wgt;
 #pragma unroll
             for (int d = 0; d < kPer; ++d) acc[d] += x.v[d] * wgt;
         }
         const int t = p.by_R.of(o.r0 + r);
-        write_row<T, D>(p, o.row0 + t, o.hk * p.R + (o.r0 + r - t * p.R), acc, top, sum);
+        write_row<T, D>(p, o.row0 + t, o.hk * p.R + (o.r0 + r - t * p.R), acc, top, settled(sum, o.len - o.n_q + t + 1 > 0));
     }
 }
 
@@ -714,19 +720,26 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         else
             cnt[kind] = c.y - c.x + 1, first[kind] = c.x, row_in[kind] = r - mb * f.M;
     }
+    // Whether the row sees anything, asked where its sums are 0 (cnt[0]: of a prefix, the same for all heads).
+    const auto sees_any = [&]() {
+        const int row0 = first_row(p, b), n_q = first_row(p, b + 1) - row0;
+        const int len = (int)min((long long)p.kv_len[b], (long long)p.table_stride << p.page_shift);
+        return cnt[0] > 0 || len - n_q + (n - row0) + 1 > 0;
+    };
     // two pieces at most, all by row: maxima and sums of the warp's heads at once
     const bool simple = kWarps == 1 && __all_sync(0xffffffffu, here && (cnt[0] == 0 || first[0] < 0) && first[1] < 0);
     if (simple) {
         const long long at = (long long)n * p.Hq + h;
         const float2 none = make_float2(-INFINITY, 0.0f), a = cnt[0] ? p.whole[0].ml[at] : none, o = p.whole[1].ml[at];
-        const float top = fmaxf(a.y > 0.0f ? a.x : -INFINITY, o.y > 0.0f ? o.x : -INFINITY);
-        const float w0 = a.y > 0.0f ? exp2_approx(a.x - top) : 0.0f, w1 = o.y > 0.0f ? exp2_approx(o.x - top) : 0.0f;
-        const float sum = a.y * w0 + o.y * w1;
+        const float top = fmaxf(a.y != 0.0f ? a.x : -INFINITY, o.y != 0.0f ? o.x : -INFINITY);
+        const float w0 = a.y != 0.0f ? exp2_approx(a.x - top) : 0.0f, w1 = o.y != 0.0f ? exp2_approx(o.x - top) : 0.0f;
+        float sum = a.y * w0 + o.y * w1;
+        if (__any_sync(0xffffffffu, sum == 0.0f)) sum = settled(sum, sees_any());
 #pragma unroll 4
         for (int i = 0; i < nh; ++i) {
             const long long row = ((long long)n * p.Hq + h0 + i) * D;
             const float u0 = __shfl_sync(0xffffffffu, w0, i), u1 = __shfl_sync(0xffffffffu, w1, i);
-            Lane<D> x, y; // (asked for before the weights are known; where a weight is 0 they may hold anything)
+            Lane<D> x, y; // (asked for before the weights are known; where a weight is 0 they may hold anything, where it is NaN the sum is)
             x.load(p.whole[0].o + row), y.load(p.whole[1].o + row);
             float acc[kPer];
 #pragma unroll
@@ -755,7 +768,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
             const float2 *ml;
             find(k, o, ml);
             const float2 v = *ml;
-            if (v.y > 0.0f) top = fmaxf(top, v.x);
+            if (v.y != 0.0f) top = fmaxf(top, v.x);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -768,7 +781,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
             const float2 v = *ml;
             Lane<D> x;
             x.load(o);
-            if (!(v.y > 0.0f)) continue; // (its sums were not written)
+            if (v.y == 0.0f) continue; // (its sums were not written)
             const float wgt = exp2_approx(v.x - top);
             sum += v.y * wgt;
 #pragma unroll
@@ -787,6 +800,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
                 sum += s_sum[w];
             }
         }
+        if (sum == 0.0f) sum = settled(sum, sees_any());
         write_row<T, D>(p, n, h0 + i, acc, top, sum);
     }
 }

@@ -583,6 +583,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             const int had_rows = my_rows, had_tiles = my_tiles, my_t = (int)(row * inv_R >> 16), my_h = row - my_t * p.R;
             const bool by_row = w->place == kToRows, at_once = by_row && p.n_groups == 0;
             const int h0 = w->hk * p.R;
+            if (at_once) l = settled(l, lim > 0);
             char *dst;             // of the engine's first row; the next token's and the next head's are so far on
             long long per_t, per_h;
             if (at_once) {
@@ -612,7 +613,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             if (had_tiles == 0 && !at_once) continue; // (where l is 0 nobody reads the sums)
             // Rows go out by way of shared memory, 128 bytes of 32 rows at a time, so that a store fills whole lines (a thread that
             // writes its own row keeps the load-store unit for 32 lines an instruction: a piece took 17000 cycles beside its tiles).
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inv = inverse(l);
             const auto out_128 = [&](const uint32_t *v, int c) { // the thread's 128 bytes, c bytes into the rows
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         tmem_wait_ld();
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = l > 0.0f ? pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv) : 0u;
+                    for (int i = 0; i < 32; ++i) v[i] = l == 0.0f ? 0u : pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
                     out_128(v, c * 2);
                 }
             } else {

@@ -507,7 +507,8 @@ class PagedCache:
         ``table`` [sequences, pages], the rows' own new tokens the last of them, and with ``prefix`` = (table [groups, pages],
         lengths [groups], cu_group [groups + 1]) the tokens that a group of sequences shares.  ``cu_q`` [sequences + 1]: ragged
         numbers of rows (None: one row per sequence).  ``scale``: None for 1 / sqrt(D).  Returns ``out`` (made if None); ``lse``, a
-        fp32 tensor [N, Hq], is filled if given."""
+        fp32 tensor [N, Hq], is filled if given.  Keys and values of visible tokens must be finite; a query that holds a NaN or an
+        infinity has a row of NaN."""
         if stream is not None:  # (what is made below is made for that stream)
             _on(stream, self.device, self._index)
             with self._torch.cuda.stream(stream):

@@ -422,6 +422,45 @@ def test_lines_of_more_than_2_30_tiles():
     assert bool(((lse[:, 0].double() - kv_len.double().log()).abs() <= 60 * 2.0**-24 + 21 * 2.0**-22).all())
 
 
+POISONED = [
+    # Hq, Hk, D, sequences, groups: whole and cut items of the narrow and the wide forms, and every way of joining
+    (4, 2, 128, [(1, 1), (1, 2), (1, 0), (1, 40)], []), (4, 1, 64, [(1, 30000)], []), (16, 16, 64, [(1, 700 + i) for i in range(300)], []),
+    (2, 1, 128, [(3, 2), (5, 9000)], []), (8, 8, 128, [(40, 400), (50, 20), (1, 1)], []), (8, 2, 64, [(120, 3000), (90, 60)], []), (4, 4, 128, [(700, 700), (300, 100)], []),
+    (8, 2, 128, [(1, 3), (1, 0), (1, 70)], [(2, 100)]), (8, 8, 64, [(1, 30)] * 80, [(40, 300), (40, 0)]), (8, 2, 64, [(9, 9), (30, 31), (12, 4)] * 10, [(15, 800), (10, 0)]),
+    (4, 4, 128, [(200, 300), (150, 0), (3, 1)], [(3, 900)]), (32, 32, 64, [(1, 5)] * 700, [(700, 50)]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("value", [NAN, math.inf, -math.inf])
+@pytest.mark.parametrize("case", POISONED, ids=lambda c: "%dx%d_d%d_n%d_g%d" % (c[0], c[1], c[2], len(c[3]), len(c[4])))
+def test_queries_that_are_not_numbers(dtype, value, case):
+    """A query that holds a NaN or an infinity has scores that are NaN or infinite (no key is zero there), and by the formula no softmax: its row
+    is NaN, log-sum too, in every form and however its pieces are joined.  Rows that see nothing stay zeros; all others are as without it."""
+    Hq, Hk, D, seqs, groups = case
+    c = Case(Hq, Hk, D, 16, dtype, seqs, groups=groups)
+    assert bool((c.k[:, :, :, 3] != 0).all())
+    want, wl, bound, lbound = c.reference(D ** -0.5)
+    bad = torch.zeros((c.n, Hq), dtype=torch.bool, device="cuda")
+    for b, (n, _) in enumerate(seqs):
+        for t in {0, n // 2, n - 1} - {-1}:
+            if (b + t) % 5 != 4:
+                bad[c.cu[b] + t, (b * 3 + t) % Hq] = True
+    c.q[..., 3] = torch.where(bad, value, c.q[..., 3])
+    lse = torch.full((c.n, Hq), 7.0, device="cuda")
+    out = c.cache.attend(c.q, c.table, c.kv_len, cu_q=c.cu_q, prefix=c.prefix, lse=lse)
+    assert c.cache.status() == dart.DART_OK
+    none = wl == -math.inf
+    assert bool((out[none] == 0).all()) and bool((lse[none] == -math.inf).all())
+    lost = bad & ~none
+    assert int(lost.sum()) > 0
+    assert bool(out[lost].isnan().all()), "%d of %d rows" % (int((~out[lost].isnan()).any(-1).sum()), int(lost.sum()))
+    assert bool(lse[lost].isnan().all())
+    some = ~bad & ~none
+    assert bool(((out.double() - want)[some].abs() <= bound[some]).all())
+    assert bool(((lse.double() - wl)[some].abs() <= lbound[some]).all())
+
+
 def test_threads_call_at_once():
     import threading
 
