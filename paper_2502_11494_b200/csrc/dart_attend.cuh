@@ -653,6 +653,14 @@ __global__ void __launch_bounds__(256) attend_join_cut_kernel(const Params p, co
     }
 }
 
+// Whether packed row n, of sequence b, sees tokens of its own.  (A function apart, of numbers: hardly any row asks, and inside the kernel it costs
+// every call's few rows some 1 us.)
+__device__ __noinline__ bool sees_own(const int32_t *cu_q, const int32_t *kv_len, int n_rows, long long most, int b, int n)
+{
+    const int row0 = cu_q ? clamp(cu_q[b], 0, n_rows) : b, n_q = cu_q ? clamp(cu_q[b + 1], 0, n_rows) - row0 : 1;
+    return (int)min((long long)kv_len[b], most) - n_q + (n - row0) + 1 > 0;
+}
+
 // Row by row: with prefixes, where nearly every row has two pieces, and for few rows, whose lists of pieces are long.  kWarps
 // warps share a row and head, or (kWarps 1) a warp takes `heads` heads of a row (at most 32).
 template <typename T, int D, int kWarps>
@@ -720,12 +728,6 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         else
             cnt[kind] = c.y - c.x + 1, first[kind] = c.x, row_in[kind] = r - mb * f.M;
     }
-    // Whether the row sees anything, asked where its sums are 0 (cnt[0]: of a prefix, the same for all heads).
-    const auto sees_any = [&]() {
-        const int row0 = first_row(p, b), n_q = first_row(p, b + 1) - row0;
-        const int len = (int)min((long long)p.kv_len[b], (long long)p.table_stride << p.page_shift);
-        return cnt[0] > 0 || len - n_q + (n - row0) + 1 > 0;
-    };
     // two pieces at most, all by row: maxima and sums of the warp's heads at once
     const bool simple = kWarps == 1 && __all_sync(0xffffffffu, here && (cnt[0] == 0 || first[0] < 0) && first[1] < 0);
     if (simple) {
@@ -734,7 +736,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         const float top = fmaxf(a.y != 0.0f ? a.x : -INFINITY, o.y != 0.0f ? o.x : -INFINITY);
         const float w0 = a.y != 0.0f ? exp2_approx(a.x - top) : 0.0f, w1 = o.y != 0.0f ? exp2_approx(o.x - top) : 0.0f;
         float sum = a.y * w0 + o.y * w1;
-        if (__any_sync(0xffffffffu, sum == 0.0f)) sum = settled(sum, sees_any());
+        if (sum == 0.0f) sum = settled(sum, cnt[0] > 0 || sees_own(p.cu_q, p.kv_len, p.n_rows, (long long)p.table_stride << p.page_shift, b, n));
 #pragma unroll 4
         for (int i = 0; i < nh; ++i) {
             const long long row = ((long long)n * p.Hq + h0 + i) * D;
@@ -800,7 +802,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
                 sum += s_sum[w];
             }
         }
-        if (sum == 0.0f) sum = settled(sum, sees_any());
+        if (sum == 0.0f) sum = settled(sum, n0 > 0 || sees_own(p.cu_q, p.kv_len, p.n_rows, (long long)p.table_stride << p.page_shift, b, n));
         write_row<T, D>(p, n, h0 + i, acc, top, sum);
     }
 }
