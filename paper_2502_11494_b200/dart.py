@@ -356,6 +356,16 @@ def _on(stream, device, index):
     return stream.cuda_stream
 
 
+def _made_for(stream):
+    """Where tensors are made that a call on ``stream`` writes or reads: the allocator hands out memory whose last user is of the stream that is
+    current, and may still be at work there."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    return torch.cuda.stream(stream)
+
+
 def _head_rows(t, name, dtype, device, n_rows, D):
     """Rows [n_rows, heads, D] with the heads of a row side by side -> (address, values from row to row, heads)."""
     shape, stride = t.shape, t.stride()
@@ -412,7 +422,7 @@ _NO_ROWS = (None, 0, 0)
 def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, out=None, stream=None):
     """Norm of each head (``q_weight`` / ``k_weight`` [D], None: no norm) and rotation of queries [N, Hq, D] and keys [N, Hk, D]
     (either may be None) in one pass.  ``pos``: int64 [N], or [axes, N].  ``out``: (q_out, k_out), which may be q and k
-    themselves.  Returns (q_out, k_out)."""
+    themselves; made for ``stream`` if None.  Returns (q_out, k_out)."""
     one = q if q is not None else k
     if one is None:
         raise ValueError("queries or keys are needed")
@@ -421,8 +431,10 @@ def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6,
     if index is None:
         raise ValueError("rows must be CUDA tensors")
     n, D = shape[0], shape[-1]
+    st = _on(stream, dev, index)
     if out is None:
-        out = tuple(t.new_empty(t.shape) if t is not None else None for t in (q, k))
+        with _made_for(stream):
+            out = tuple(t.new_empty(t.shape) if t is not None else None for t in (q, k))
     q_out, k_out = out
     qa = _head_rows(q, "q", dtype, dev, n, D) if q is not None else _NO_ROWS
     ka = _head_rows(k, "k", dtype, dev, n, D) if k is not None else _NO_ROWS
@@ -438,7 +450,7 @@ def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6,
         turn = rope.at(pos, n, dev)
     rc = lib().dart_norm_rope(qa[0], qa[1], qa[2], ka[0], ka[1], ka[2], n, D, code, _vector(q_weight, "q_weight", D, dtype, dev),
                               _vector(k_weight, "k_weight", D, dtype, dev), eps, turn[0], turn[1], turn[2], qo[0], qo[1], ko[0], ko[1], index,
-                              _on(stream, dev, index))
+                              st)
     if rc != DART_OK:
         raise DartError(rc, "dart_norm_rope")
     return out

@@ -313,3 +313,33 @@ def test_captured_and_replayed():
         for b in range(4):
             assert torch.equal(kc[table[b, step // 16], :, step % 16], want[b]) and torch.equal(vc[table[b, step // 16], :, step % 16], k[b])
     assert cache.status() == dart.DART_OK and math.isfinite(float(out.float().sum()))
+
+
+def _busy_block(nbytes):
+    """A block of the current stream's that is free again, but whose last user is still to come: behind some 50 ms of nothing."""
+    t = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)
+    t.fill_(7)
+    return t.data_ptr()
+
+
+def test_outputs_are_made_on_the_stream_that_writes_them():
+    """With stream= and no out=: memory that the current stream has freed but not finished with is not handed to another stream."""
+    n, Hq, Hk, D = 4096, 8, 2, 128
+    g = _gen(3)
+    q, k = torch.randn((n, Hq, D), generator=g, device="cuda").to(torch.bfloat16), torch.randn((n, Hk, D), generator=g, device="cuda").to(torch.bfloat16)
+    rope, pos = dart.Rope(_inv_freq(D)), torch.arange(n, device="cuda")
+    want = dart.norm_rope(q, k, pos=pos, rope=rope)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        blocks = {_busy_block(q.numel() * 2), _busy_block(k.numel() * 2)}
+        got = dart.norm_rope(q, k, pos=pos, rope=rope, stream=s)
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and not {t.data_ptr() for t in got} & blocks
+        del got
+    q_only, none = dart.norm_rope(q, None, pos=pos, rope=rope, stream=s)
+    s.synchronize()
+    assert none is None and torch.equal(q_only, want[0])
