@@ -249,8 +249,18 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _made_for(stream):
+    """Where tensors are made that a call on ``stream`` writes or reads: the allocator hands out memory whose last user is of the stream that is
+    current, and may still be at work there."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    return torch.cuda.stream(stream)
+
+
 class Dart:
-    """A reduction context bound to one CUDA device.  ``reduce`` enqueues on torch's current stream."""
+    """A reduction context bound to one CUDA device.  ``reduce`` enqueues on torch's current stream, or on ``stream``."""
 
     def __init__(self, B_max, S_max, d, P_max, Kp_max, device=0, flags=0):
         rc, self._h = dart_create(B_max, S_max, d, P_max, Kp_max, device, flags)
@@ -295,21 +305,23 @@ class Dart:
         if out is None:
             if not (0 < n_keep <= n_vis <= S):
                 raise DartError(DART_ERR_BAD_SHAPE, "dart_reduce")
-            out = (torch.empty((B, S_out, d), dtype=torch.bfloat16, device=dev),
-                   torch.empty((B, S_out), dtype=torch.int32, device=dev),
-                   torch.empty((B, S_out), dtype=torch.int64, device=dev))
+            with _made_for(stream):
+                out = (torch.empty((B, S_out, d), dtype=torch.bfloat16, device=dev),
+                       torch.empty((B, S_out), dtype=torch.int32, device=dev),
+                       torch.empty((B, S_out), dtype=torch.int64, device=dev))
         oh, oi, op = out
         dbg_t, dbg_s = None, None
         if debug:
-            dbg_t = {
-                "l1": torch.empty((B, n_vis), dtype=torch.float32, device=dev),
-                "ssq": torch.empty((B, n_vis), dtype=torch.float32, device=dev),
-                "pivot_idx": torch.empty((B, n_pivot), dtype=torch.int32, device=dev),
-                "sim": torch.empty((B, n_pivot, n_vis), dtype=torch.float32, device=dev),
-                "eps": torch.empty((B, n_pivot), dtype=torch.float32, device=dev),
-                "keep": torch.empty((B, n_vis), dtype=torch.uint8, device=dev),
-                "owner": torch.empty((B, n_vis), dtype=torch.int32, device=dev),
-            }
+            with _made_for(stream):
+                dbg_t = {
+                    "l1": torch.empty((B, n_vis), dtype=torch.float32, device=dev),
+                    "ssq": torch.empty((B, n_vis), dtype=torch.float32, device=dev),
+                    "pivot_idx": torch.empty((B, n_pivot), dtype=torch.int32, device=dev),
+                    "sim": torch.empty((B, n_pivot, n_vis), dtype=torch.float32, device=dev),
+                    "eps": torch.empty((B, n_pivot), dtype=torch.float32, device=dev),
+                    "keep": torch.empty((B, n_vis), dtype=torch.uint8, device=dev),
+                    "owner": torch.empty((B, n_vis), dtype=torch.int32, device=dev),
+                }
             dbg_s = dart_debug(**{k: v.data_ptr() for k, v in dbg_t.items()})
         st = stream if stream is not None else torch.cuda.current_stream(dev)
         rc = dart_reduce_ex(self._h, _ptr(hidden), _ptr(keys), _ptr(pos_in), vis_offset, n_vis, n_pivot, n_keep,
@@ -354,16 +366,6 @@ def _on(stream, device, index):
     if stream.device != device:
         raise ValueError("the stream must be of the rows' device")
     return stream.cuda_stream
-
-
-def _made_for(stream):
-    """Where tensors are made that a call on ``stream`` writes or reads: the allocator hands out memory whose last user is of the stream that is
-    current, and may still be at work there."""
-    if stream is None:
-        return contextlib.nullcontext()
-    import torch
-
-    return torch.cuda.stream(stream)
 
 
 def _head_rows(t, name, dtype, device, n_rows, D):

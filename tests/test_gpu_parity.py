@@ -539,3 +539,28 @@ def test_a_failed_allocation_is_reported_once():
     torch.cuda.synchronize()
     assert ctx.status() == dart.DART_OK
     ctx.close()
+
+
+def test_reduce_makes_its_outputs_on_the_stream_that_writes_them():
+    """With stream= and no out=: memory that the current stream has freed but not finished with is not handed to another stream."""
+    w = W.LLAVA15_B64.with_(B=16)
+    keys, hidden = W.make_batch(w, device="cuda:0")
+    ctx = dart.Dart(w.B, w.S, w.d, w.n_pivot, w.n_keep, device=0)
+    args = (hidden, keys, w.vis_offset, w.n_vis, w.n_pivot, w.n_keep)
+    want = ctx.reduce(*args)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(2):
+        torch.cuda.empty_cache()
+        block = torch.empty_like(want[0])
+        torch.cuda.synchronize()
+        torch.cuda._sleep(100_000_000)  # some 50 ms
+        block.fill_(7)
+        at = block.data_ptr()
+        del block  # free again, but its last user is still to come
+        got = ctx.reduce(*args, stream=s)
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert got[0].data_ptr() != at and all(torch.equal(a, b) for a, b in zip(got, want)) and ctx.status() == dart.DART_OK
+        del got
+    ctx.close()
