@@ -507,7 +507,8 @@ class PagedCache:
             turn = _NO_ROPE
         else:
             if pos is not None and rope.axes == 1 and pos.dim() > 1:
-                pos = pos.reshape(-1)
+                with _made_for(stream):  # (positions that lie apart are copied)
+                    pos = pos.reshape(-1)
             turn = rope.at(pos, n, dev)
         rc = lib().dart_cache_append(self._c, ka[0], ka[1], va[0], va[1], n_seq, n, self._ints(cu_rows, "cu_rows", n_seq + 1), self._ints(idx, "idx"),
                                      S, tp, ts, self._ints(start, "start", n_seq), _vector(k_weight, "k_weight", D, dtype, dev), eps,

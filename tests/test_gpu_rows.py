@@ -343,3 +343,27 @@ def test_outputs_are_made_on_the_stream_that_writes_them():
     q_only, none = dart.norm_rope(q, None, pos=pos, rope=rope, stream=s)
     s.synchronize()
     assert none is None and torch.equal(q_only, want[0])
+
+
+def test_positions_are_copied_on_the_stream_that_reads_them():
+    """Positions [B, S_out] that lie apart are copied for the call, on the call's stream: a copy queued behind the current stream's work would be
+    read before it is made."""
+    B, S_out, Hk, D, page = 2, 300, 2, 64, 16
+    g = _gen(4)
+    k, v = _rows((B * S_out, Hk, D), torch.bfloat16, g), _rows((B * S_out, Hk, D), torch.bfloat16, g)
+    pages = B * ((S_out + page - 1) // page)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(B, -1)
+    wide = torch.randint(0, 5000, (B, S_out + 7), generator=g, device="cuda")
+    rope, s = dart.Rope(_inv_freq(D)), torch.cuda.Stream()
+    results = []
+    for stream in (None, s):
+        kc = torch.zeros((pages, Hk, page, D), dtype=torch.bfloat16, device="cuda")
+        cache = dart.PagedCache(kc, torch.zeros_like(kc))
+        torch.cuda.synchronize()
+        if stream is not None:
+            torch.cuda._sleep(100_000_000)  # some 50 ms
+        cache.append(k, v, table, pos=wide[:, :S_out], rope=rope, stream=stream)
+        torch.cuda.synchronize()
+        assert cache.status() == dart.DART_OK
+        results.append(kc)
+    assert torch.equal(*results)
