@@ -455,7 +455,7 @@ typedef struct {
                                      cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
                                      that do not ascend name more rows than there are, or the work has 2^31 pairs of a tile of rows and a tile of tokens or
                                      more (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
-                                     status[1..3] say which wait, item and CTA */
+                                     status[1..3] say which wait, item and CTA.  A status that is not 0 stays, but for TIMEOUT over CHECK */
     int32_t test_withhold;        /* testing only: 1 withholds one hand-over inside the kernel that waits, 2 lets the wait for a tile's queries
                                      give up at once, while their copy may still be under way */
 } dart_attend_args;

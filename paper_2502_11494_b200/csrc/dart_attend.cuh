@@ -23,7 +23,6 @@
 namespace dart {
 namespace attend {
 
-constexpr int kErrCheck = -8;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // Division by a number that the host knows, for n < 2^31: a multiplication and a shift (Granlund and Montgomery's method: with
@@ -85,6 +84,8 @@ __device__ __forceinline__ int clamp(int x, int lo, int hi) { return min(max(x, 
 // First packed row of sequence b.  (Offsets that do not ascend are held inside the rows: nothing out of bounds is touched.)
 __device__ __forceinline__ int first_row(const Params &p, int b) { return p.cu_q ? clamp(p.cu_q[b], 0, p.n_rows) : b; }
 
+// (kReport: the plan's first look at a segment, for all that come after it)
+template <bool kReport = false>
 __device__ inline Seg load_seg(const Params &p, int s)
 {
     Seg g;
@@ -101,7 +102,7 @@ __device__ inline Seg load_seg(const Params &p, int s)
     g.n_q = max(first_row(p, b1) - g.row0, 0);
     const long long most = (long long)g.width << p.page_shift;
     if (g.len < 0 || g.len > most) {
-        if (p.status) *p.status = kErrCheck;
+        if (kReport) report_check(p.status);
         g.len = g.len < 0 ? 0 : (int)most;
     }
     g.nmb = g.prefix && g.len == 0 ? 0 : p.pieces.by_M.of(g.n_q * p.R + p.pieces.M - 1);
@@ -159,7 +160,7 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
     Seg g;
 #pragma unroll 1
     for (int s = s0; s < s1; ++s) {
-        g = load_seg(p, s);
+        g = load_seg<true>(p, s);
         items += p.Hk * (long long)g.nmb, room += room_of<kTile, kCost>(p, g);
     }
     long long i_sum = items, r_sum = room;
@@ -180,7 +181,7 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
     const Shares share = Shares::of(ok ? (int)r_all : 0, i_all, p.n_workers, p.least);
     if (tid == 0) {
         sh.share = share;
-        if (!ok && p.status) *p.status = kErrCheck;
+        if (!ok) report_check(p.status);
     }
     if (ok && room > 0) {
         const int begin = (int)(r_sum - room), end = (int)r_sum; // the thread's part of the line
@@ -376,7 +377,7 @@ struct Feed {
             pages = w.g.table[i];
             if (pages < 0 || pages >= p.n_pages) {
                 pages = -1; // reads as zeros
-                if (p.status) *p.status = kErrCheck;
+                report_check(p.status);
             }
         }
     }

@@ -91,6 +91,14 @@ __device__ __forceinline__ bool asleep_until(uint32_t bar, uint32_t parity)
 }
 struct Waits {
     sweep::Ctl ctl;
+    // Rows that are not valid say more than a page that read as zeros: the status becomes TIMEOUT over CHECK too.
+    __device__ void give_up(int where, long long task) const
+    {
+        *ctl.abort_flag = 1;
+        int was = atomicCAS(ctl.status, 0, sweep::kStatusTimeout);
+        if (was == kErrCheck && atomicCAS(ctl.status, kErrCheck, sweep::kStatusTimeout) == kErrCheck) was = 0;
+        if (was == 0) ctl.status[1] = where, ctl.status[2] = (int)task, ctl.status[3] = (int)blockIdx.x;
+    }
     __device__ bool wait_bar(uint32_t bar, uint32_t parity, int where, long long task) const
     {
         if (asleep_until(bar, parity)) return true;
@@ -98,7 +106,7 @@ struct Waits {
         while (!asleep_until(bar, parity)) {
             if (ctl.aborted()) return false;
             if ((unsigned long long)(clock64() - t0) > ctl.limit_cycles) {
-                ctl.give_up(where, task);
+                give_up(where, task);
                 return false;
             }
         }
@@ -289,7 +297,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                     if (tile >= w.b || lane * box >= kWideTile || tok >= w.vis) return nowhere;
                     const int pg = w.g.table[tok >> p.page_shift];
                     if (pg < 0 || pg >= p.n_pages) {
-                        if (p.status) *p.status = kErrCheck;
+                        report_check(p.status);
                         return nowhere; // reads as zeros
                     }
                     return ((pg * p.Hk + w.hk) << p.page_shift) + (tok & ((1 << p.page_shift) - 1));
@@ -361,7 +369,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};
             const auto queries = [&](int e) { // a piece's queries are there
                 if (withhold == 2) {
-                    if (issues) ctl.ctl.give_up(kWaitQueries, -1);
+                    if (issues) ctl.give_up(kWaitQueries, -1);
                     __syncwarp();
                     return false;
                 }

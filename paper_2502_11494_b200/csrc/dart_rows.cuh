@@ -23,7 +23,6 @@ namespace rows {
 constexpr int kThreads = 128;
 constexpr int kMaxRows = 8;      // rows per block
 constexpr int kMaxHalf = 128;    // rotated pairs of a head (head_dim <= 256)
-constexpr int kErrCheck = -8;    // status: an index or a page outside its range
 
 // One kind of row: queries, keys or values.
 struct Side {
@@ -120,7 +119,7 @@ __device__ __forceinline__ Place place_of(const Params &p, int n)
     if (slot >= 0 && col < p.table_stride) page = p.table[(long long)b * p.table_stride + col];
     const long long src = p.idx ? (long long)p.idx[n] : n;
     if (page < 0 || page >= p.n_pages || (p.idx && (src < 0 || src >= p.S))) {
-        if (p.status) *p.status = kErrCheck;
+        report_check(p.status);
         return r;
     }
     r.src = p.idx ? (long long)b * p.S + src : src;

@@ -461,6 +461,48 @@ def test_queries_that_are_not_numbers(dtype, value, case):
     assert bool(((lse.double() - wl)[some].abs() <= lbound[some]).all())
 
 
+@pytest.mark.parametrize("before", [dart.DART_OK, dart.DART_ERR_CHECK])
+@pytest.mark.parametrize("bad_page", [False, True])
+@pytest.mark.parametrize("withhold", [1, 2])
+def test_a_wait_that_runs_out_says_more_than_a_bad_page(withhold, bad_page, before):
+    """TIMEOUT (rows are not valid) over CHECK (a page read as zeros), in whichever order they come."""
+    c = Case(8, 2, 128, 16, "bf16", [(40, 400)] * 3)
+    if bad_page:
+        c.table[:, 7] = -1
+    status = torch.tensor([before, 0, 0, 0], dtype=torch.int32, device="cuda")
+    p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    out = torch.zeros((c.n, 8, 128), dtype=torch.bfloat16, device="cuda")
+    a = dart.dart_attend_args(p(c.q), p(out), None, c.q.stride(0), out.stride(0), c.n, 8, 3, 0, p(c.cu_q), p(c.table), p(c.kv_len), None, None, None, c.table.stride(0), 0,
+                              128 ** -0.5, 20000, p(status), withhold)
+    need = dart.dart_attend_workspace(c.cache._c, a)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    assert dart.dart_attend(c.cache._c, a, p(ws), need, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == dart.DART_OK
+    torch.cuda.synchronize()
+    got = status.tolist()
+    assert got[0] == dart.DART_ERR_TIMEOUT and 110 <= got[1] <= 125, got
+
+
+def test_what_a_call_reports_does_not_hide_a_wait_that_ran_out():
+    """A cache's status word is shared by its calls: rows left out, pages that read as zeros, lengths that are cut and offsets that cannot be come
+    after a TIMEOUT that nobody has read."""
+    c = Case(4, 2, 128, 16, "bf16", [(1, 100), (1, 40)])
+    wide = Case(4, 2, 128, 16, "bf16", [(40, 100), (40, 40)])
+    rows = torch.zeros((2, 2, 128), dtype=torch.bfloat16, device="cuda")
+    bad = torch.full_like(c.table, -1)
+    long = torch.full_like(c.kv_len, 1 << 20)
+    none = torch.zeros_like(c.table)
+    calls = [
+        lambda: c.cache.append(rows, rows, bad), lambda: c.cache.attend(c.q, bad, c.kv_len), lambda: c.cache.attend(c.q, none, long), lambda: c.cache.attend(c.q, none, -long),
+        lambda: c.cache.attend(wide.q, torch.full_like(wide.table, -1)[:, :c.table.shape[1]].contiguous(), wide.kv_len, cu_q=wide.cu_q),
+    ]
+    for call in calls:
+        call()
+        assert c.cache.status() == dart.DART_ERR_CHECK  # (each of them does report)
+        c.cache._status[0] = dart.DART_ERR_TIMEOUT
+        call()
+        assert c.cache.status() == dart.DART_ERR_TIMEOUT and c.cache.status() == dart.DART_OK
+
+
 def test_threads_call_at_once():
     import threading
 
