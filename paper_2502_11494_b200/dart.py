@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import threading
 from typing import Optional
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -471,6 +472,7 @@ class PagedCache:
         self.heads, self.head_dim, self._index = k.shape[1], k.shape[3], k.device.index
         self._status = torch.zeros(4, dtype=torch.int32, device=k.device)
         self._status_at, self._int32, self._torch = self._status.data_ptr(), torch.int32, torch
+        self._lock = threading.Lock()  # held by a launch, and by status() from its waiting to its clearing
         self._c = dart_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3], _code(k.dtype), self._index)
 
     def _ints(self, t, name, size=None):
@@ -510,10 +512,11 @@ class PagedCache:
                 with _made_for(stream):  # (positions that lie apart are copied)
                     pos = pos.reshape(-1)
             turn = rope.at(pos, n, dev)
-        rc = lib().dart_cache_append(self._c, ka[0], ka[1], va[0], va[1], n_seq, n, self._ints(cu_rows, "cu_rows", n_seq + 1), self._ints(idx, "idx"),
-                                     S, tp, ts, self._ints(start, "start", n_seq), _vector(k_weight, "k_weight", D, dtype, dev), eps,
-                                     turn[0], turn[1], turn[2], self._status_at,
-                                     _on(stream, dev, self._index))
+        args = (self._c, ka[0], ka[1], va[0], va[1], n_seq, n, self._ints(cu_rows, "cu_rows", n_seq + 1), self._ints(idx, "idx"), S, tp, ts,
+                self._ints(start, "start", n_seq), _vector(k_weight, "k_weight", D, dtype, dev), eps, turn[0], turn[1], turn[2], self._status_at,
+                _on(stream, dev, self._index))
+        with self._lock:
+            rc = lib().dart_cache_append(*args)
         if rc != DART_OK:
             raise DartError(rc, "dart_cache_append")
 
@@ -551,16 +554,20 @@ class PagedCache:
         # (made for this call on its stream: the allocator keeps it apart from other streams' and graphs' calls)
         need = L.dart_attend_workspace(self._c, a)
         ws = self._torch.empty(need, dtype=self._torch.uint8, device=dev) if need else None
-        rc = L.dart_attend(self._c, a, ws.data_ptr() if need else None, need, _raw_stream(self._index))
+        with self._lock:
+            rc = L.dart_attend(self._c, a, ws.data_ptr() if need else None, need, _raw_stream(self._index))
         if rc != DART_OK:
             raise DartError(rc, "dart_attend")
         return out
 
     def status(self) -> int:
-        """DART_OK, or what a kernel found wrong since the last reading (a page or an index out of range, a wait that gave up).
-        Waits for the device; reading clears it."""
-        self._torch.cuda.synchronize(self.device)
-        code = int(self._status[0].item())
-        if code:
-            self._status.zero_()
+        """DART_OK, or what a kernel found wrong since the last reading (a page or an index out of range, a wait that gave up), in any call
+        and on any stream: the caller tells them apart by reading in between.  Waits for the device; reading clears it, and calls of other threads
+        wait until it has (replays of captured graphs do not: read between them)."""
+        with self._lock:
+            self._torch.cuda.synchronize(self.device)
+            code = int(self._status[0].item())
+            if code:
+                self._status.zero_()
+                self._torch.cuda.synchronize(self.device)  # (before a call on another stream reports)
         return code

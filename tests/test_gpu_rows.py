@@ -367,3 +367,38 @@ def test_positions_are_copied_on_the_stream_that_reads_them():
         assert cache.status() == dart.DART_OK
         results.append(kc)
     assert torch.equal(*results)
+
+
+def _bad_append(cache, **kw):
+    rows = torch.zeros((2, cache.heads, cache.head_dim), dtype=cache.dtype, device="cuda")
+    cache.append(rows, rows, torch.full((2, 1), -1, dtype=torch.int32, device="cuda"), **kw)
+
+
+def test_reports_of_other_threads_are_not_lost():
+    """Another thread's call comes between the reading of the status and its clearing: what it reports is read the next time."""
+    import threading
+
+    k = torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+    cache = dart.PagedCache(k, torch.zeros_like(k))
+
+    class Word:
+        """The status word; before it is cleared the other thread gets half a second to report."""
+
+        def __init__(self, t):
+            self.t, self.thread = t, None
+
+        def __getitem__(self, i):
+            return self.t[i]
+
+        def zero_(self):
+            self.thread = threading.Thread(target=lambda: (_bad_append(cache), torch.cuda.synchronize()))
+            self.thread.start()
+            self.thread.join(0.5)
+            return self.t.zero_()
+
+    word = cache._status = Word(cache._status)
+    _bad_append(cache)
+    assert cache.status() == dart.DART_ERR_CHECK
+    word.thread.join()
+    cache._status = word.t
+    assert cache.status() == dart.DART_ERR_CHECK and cache.status() == dart.DART_OK
