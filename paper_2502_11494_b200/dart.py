@@ -471,6 +471,9 @@ class PagedCache:
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self.heads, self.head_dim, self._index = k.shape[1], k.shape[3], k.device.index
         self._status = torch.zeros(4, dtype=torch.int32, device=k.device)
+        with torch.cuda.device(k.device):  # (cleared before a call on another stream reports; a capture clears it by itself)
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()
         self._status_at, self._int32, self._torch = self._status.data_ptr(), torch.int32, torch
         self._lock = threading.Lock()  # held by a launch, and by status() from its waiting to its clearing
         self._c = dart_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3], _code(k.dtype), self._index)

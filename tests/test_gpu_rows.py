@@ -402,3 +402,18 @@ def test_reports_of_other_threads_are_not_lost():
     word.thread.join()
     cache._status = word.t
     assert cache.status() == dart.DART_ERR_CHECK and cache.status() == dart.DART_OK
+
+
+def test_a_new_cache_can_be_used_on_another_stream_at_once():
+    """The status word is cleared before the first call may report, whatever the stream that was current has still to do."""
+    k = torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+    v, s = torch.zeros_like(k), torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        _bad_append(dart.PagedCache(k, v))  # (memory of the stream's own is there: asking the device for some would wait)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)  # some 50 ms
+    cache = dart.PagedCache(k, v)
+    with torch.cuda.stream(s):
+        _bad_append(cache)
+    s.synchronize()
+    assert cache.status() == dart.DART_ERR_CHECK and cache.status() == dart.DART_OK
