@@ -485,12 +485,18 @@ class PagedCache:
             raise ValueError("%s must be contiguous int32%s on %s" % (name, " [%d]" % size if size is not None else "", self.device))
         return t.data_ptr()
 
-    def _table(self, t, name):
+    def _table(self, t, name, stream=None):
+        """(address, entries from row to row, rows, what has to live until the launch).  The rows of a view are as wide as its stride for the
+        kernels, which look at lengths against that: a view whose last row ends beyond its memory is copied."""
         shape, stride = t.shape, t.stride()
         if (t.dtype is not self._int32 or t.device != self.device or len(shape) != 2 or (shape[1] > 1 and stride[1] != 1)
                 or (shape[0] > 1 and stride[0] < shape[1])):
             raise ValueError("%s must be int32 [sequences, pages] on %s" % (name, self.device))
-        return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1], shape[0]
+        if shape[0] > 1 and stride[0] > shape[1] and 4 * (t.storage_offset() + shape[0] * stride[0]) > t.untyped_storage().nbytes():
+            with _made_for(stream):
+                t = t.contiguous()
+            stride = t.stride()
+        return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1], shape[0], t
 
     def append(self, k, v, table, start=None, cu_rows=None, idx=None, S=0, pos=None, rope=None, k_weight=None, eps=1e-6, stream=None):
         """Rows of keys and values [N, heads, D] behind the ``start`` tokens that each sequence already has.  ``cu_rows``
@@ -498,7 +504,7 @@ class PagedCache:
         b * S + idx[n] for packed row n.  The keys are normalised (``k_weight``) and rotated (``rope``, at ``pos`` or at the slots)
         on the way."""
         dev, dtype, D = self.device, self.dtype, self.head_dim
-        tp, ts, n_seq = self._table(table, "table")
+        tp, ts, n_seq, table = self._table(table, "table", stream)
         rows = k.shape[0]
         ka, va = _head_rows(k, "k", dtype, dev, rows, D), _head_rows(v, "v", dtype, dev, rows, D)
         if ka[2] != self.heads or va[2] != self.heads:
@@ -544,12 +550,12 @@ class PagedCache:
             raise ValueError("out must have q's heads")
         if lse is not None and not (lse.dtype is self._torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == dev):
             raise ValueError("lse must be contiguous fp32 [rows, heads] on the rows' device")
-        tp, ts, n_seq = self._table(table, "table")
+        tp, ts, n_seq, table = self._table(table, "table")
         if prefix is not None:
-            pp, ps, groups = self._table(prefix[0], "prefix table")
+            pp, ps, groups, ptable = self._table(prefix[0], "prefix table")
             pl, cg = self._ints(prefix[1], "prefix lengths", groups), self._ints(prefix[2], "cu_group", groups + 1)
         else:
-            pp, ps, groups, pl, cg = None, 0, 0, None, None
+            pp, ps, groups, ptable, pl, cg = None, 0, 0, None, None, None
         a = dart_attend_args(qa[0], oa[0], lse.data_ptr() if lse is not None else None, qa[1], oa[1], n, qa[2], n_seq, groups,
                              self._ints(cu_q, "cu_q", n_seq + 1), tp, self._ints(kv_len, "kv_len", n_seq), cg, pp, pl, ts, ps,
                              D ** -0.5 if scale is None else scale, wait_limit, self._status_at)

@@ -503,6 +503,29 @@ def test_what_a_call_reports_does_not_hide_a_wait_that_ran_out():
         assert c.cache.status() == dart.DART_ERR_TIMEOUT and c.cache.status() == dart.DART_OK
 
 
+def test_tables_that_are_the_last_columns_of_wider_ones():
+    """The table of a view whose last row ends beyond its memory is copied on the call's stream; a length that is longer than its row is cut there."""
+    c = Case(4, 2, 64, 16, "fp16", [(1, 100), (1, 40)], groups=[(2, 70)])
+    want = c.check()[0].clone()
+    views = []
+    for t in (c.table, c.ptable):
+        wide = torch.full((t.shape[0], t.shape[1] + 5), 2**30, dtype=torch.int32, device="cuda")
+        wide[:, 5:] = t
+        views.append(wide[:, 5:])
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, s):
+        torch.cuda._sleep(10_000_000)
+        out = c.cache.attend(c.q, views[0], c.kv_len, prefix=(views[1], *c.prefix[1:]), stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and c.cache.status() == dart.DART_OK
+    c.k.nan_to_num_(0.0), c.v.nan_to_num_(0.0)
+    views[0][views[0] >= c.k.shape[0]] = 0
+    out = c.cache.attend(c.q, views[0], torch.full_like(c.kv_len, 16 * views[0].shape[1] + 1), prefix=(views[1], *c.prefix[1:]))
+    cut = c.cache.attend(c.q, views[0].contiguous(), torch.full_like(c.kv_len, 16 * views[0].shape[1]), prefix=c.prefix)
+    assert c.cache.status() == dart.DART_ERR_CHECK and torch.equal(out, cut)
+
+
 def test_threads_call_at_once():
     import threading
 

@@ -134,3 +134,20 @@ def test_attend_wants_its_workspace(dart):
     assert _attend(dart, n_rows=0, cu_q=A) == (dart.DART_OK, 0) and _attend(dart, **GROUPS)[1] > need
     assert dart.dart_attend(None, None, None, 0, None) == dart.DART_ERR_NULL
     assert ctypes.sizeof(dart.dart_attend_args) == 136 and dart.dart_attend_args.scale.offset == 112 and dart.dart_attend_args.status.offset == 120
+
+
+def test_rows_of_a_table_end_inside_its_memory(dart):
+    """The kernels take a row of a table for as wide as its stride, and cut lengths at that: columns of a wider table from the first one on are
+    taken as they lie, later ones, whose last row would end beyond the memory, are copied."""
+    torch = pytest.importorskip("torch")
+    cache = object.__new__(dart.PagedCache)
+    cache._int32, cache.device = torch.int32, torch.device("cpu")
+    wide = torch.arange(40, dtype=torch.int32).view(4, 10)
+    views = [wide, wide[:, :6], wide[:, 5:], wide[1:, 3:], wide[:3, 5:], wide[3:, 2:5], wide[:, 9:], wide.view(-1)[2:38].view(4, 9), wide[::2], wide[::3, 4:]]
+    copied = []
+    for v in views:
+        at, stride, rows, keep = cache._table(v, "table")
+        end = keep.untyped_storage().data_ptr() + keep.untyped_storage().nbytes()
+        assert rows == v.shape[0] and at == keep.data_ptr() and at + 4 * stride * rows <= end and stride >= v.shape[1] and torch.equal(keep, v)
+        copied.append(at != v.data_ptr())
+    assert copied == [False, False, True, True, False, False, True, False, False, True]
