@@ -74,7 +74,7 @@ int launch_rows(dart::rows::Params &p, cudaStream_t st)
         p.heads_per_block = H < groups ? H : groups;
     else
         while (p.rows_per_block < kMaxRows && p.rows_per_block * H < 8 * groups) p.rows_per_block *= 2;
-    const dim3 grid((unsigned)((p.n_rows + p.rows_per_block - 1) / p.rows_per_block), (unsigned)((H + p.heads_per_block - 1) / p.heads_per_block));
+    const dim3 grid((unsigned)((p.n_rows - 1) / p.rows_per_block + 1), (unsigned)((H + p.heads_per_block - 1) / p.heads_per_block));
     if (grid.y > 65535u) return DART_ERR_BAD_SHAPE;
     cudaError_t e = kh == 4    ? launch_next(head_rows_kernel<T, 4, kPaged>, grid, kThreads, 0, st, p)
                     : kh == 8  ? launch_next(head_rows_kernel<T, 8, kPaged>, grid, kThreads, 0, st, p)

@@ -417,3 +417,18 @@ def test_a_new_cache_can_be_used_on_another_stream_at_once():
         _bad_append(cache)
     s.synchronize()
     assert cache.status() == dart.DART_ERR_CHECK and cache.status() == dart.DART_OK
+
+
+def test_as_many_rows_as_there_are_numbers():
+    """2^31 - 1 rows of one head of 8, in place: 34 GB, rows counted up to the largest number that n_rows can be."""
+    n = 2**31 - 1
+    rows = torch.zeros((n, 1, 8), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, 7, 8, 2**30 + 5, n - 9, n - 8, n - 7, n - 2, n - 1], device="cuda")
+    x = _rows((len(at), 1, 8), torch.bfloat16, _gen(9))
+    rows[at] = x
+    w = torch.arange(1, 9, device="cuda").to(torch.bfloat16)
+    q, none = dart.norm_rope(rows, None, q_weight=w, eps=1e-6, out=(rows, None))
+    torch.cuda.synchronize()
+    assert q is rows and none is None
+    close(rows[at], *reference(x, w, 1e-6, None, None, None, False))
+    assert bool((rows[2:7] == 0).all()) and bool((rows[n - 6:n - 2] == 0).all())
