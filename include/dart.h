@@ -380,7 +380,9 @@ typedef struct {
 
 /*
  * The norm of every head of the queries and keys and their rotation, in one pass: y = x * rsqrt(mean(x^2) + eps) * weight, then the
- * rotation.  The keys' rows, heads side by side, are what dart_reduce scores.
+ * rotation.  The keys' rows, heads side by side, are what dart_reduce scores (bf16 only): as its keys, where they are as wide as the hidden rows; where
+ * they are narrower (fewer key heads than query heads), as the rows of a context of their width with keys NULL, whose out_idx then packs the hidden
+ * rows with dart_gather_rows.
  *   q, k           [n_rows] rows of n_q_heads / n_k_heads heads, device, 16-byte aligned; either may have 0 heads (then its
  *                  pointers are not looked at)
  *   q_weight, k_weight [head_dim] of the rows' type, device, 16-byte aligned, or NULL: no norm

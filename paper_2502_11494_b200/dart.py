@@ -425,7 +425,10 @@ _NO_ROWS = (None, 0, 0)
 def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, out=None, stream=None):
     """Norm of each head (``q_weight`` / ``k_weight`` [D], None: no norm) and rotation of queries [N, Hq, D] and keys [N, Hk, D]
     (either may be None) in one pass.  ``pos``: int64 [N], or [axes, N].  ``out``: (q_out, k_out), which may be q and k
-    themselves; made for ``stream`` if None.  Returns (q_out, k_out)."""
+    themselves; made for ``stream`` if None.  Returns (q_out, k_out).
+
+    The keys are what ``Dart.reduce`` scores (bf16): ``reduce(hidden, keys)`` where they are as wide as the hidden rows; with fewer key heads
+    ``reduce(keys, None)``, and ``dart_gather_rows`` packs the hidden rows by its index list."""
     one = q if q is not None else k
     if one is None:
         raise ValueError("queries or keys are needed")

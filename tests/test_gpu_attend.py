@@ -599,3 +599,35 @@ def test_from_projection_to_answer():
             assert bool((off <= bound).all()) and float(x.norm(dim=-1).max() * K.norm(dim=-1).max()) / 8 < 20
     assert torch.equal(out_hidden, torch.gather(hidden, 1, idx.long()[..., None].expand(-1, -1, Hk * D)))
     ctx.close()
+
+
+def test_keys_of_grouped_heads_are_reduced_by_themselves():
+    """Fewer key heads than query heads: keys narrower than the hidden rows.  The reduction takes the keys as its rows, its index list then packs the
+    hidden rows and names the rows that go into pages."""
+    B, S, Hq, Hk, D, P, Kp, vo, nv = 3, 240, 8, 2, 64, 4, 40, 20, 200
+    g = _gen(5)
+    rows = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    rope = dart.Rope((1.0 / 10000.0 ** (torch.arange(0, D, 2, dtype=torch.float64) / D)).float().cuda())
+    hidden, k, v = rows(B, S, Hq * D), rows(B * S, Hk, D), rows(B * S, Hk, D)
+    pos = torch.arange(S, device="cuda").repeat(B)
+    _, keys = dart.norm_rope(None, k, pos=pos, rope=rope)
+    ctx = dart.Dart(B, S, Hk * D, P, Kp)
+    kept_keys, idx, out_pos = ctx.reduce(keys.view(B, S, Hk * D), None, vo, nv, P, Kp)
+    S_out = S - nv + Kp
+    out_hidden = torch.empty((B, S_out, Hq * D), dtype=torch.bfloat16, device="cuda")
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert dart.dart_gather_rows(hidden.data_ptr(), ctypes.cast(idx.data_ptr(), ctypes.POINTER(ctypes.c_int32)), B, S, S_out, 2 * Hq * D, out_hidden.data_ptr(), 0,
+                                 stream) == dart.DART_OK
+    per = (S_out + 15) // 16
+    kc, vc = rows(B * per, Hk, 16, D), rows(B * per, Hk, 16, D)
+    table = torch.randperm(B * per, generator=g, device="cuda").to(torch.int32).view(B, per)
+    cache = dart.PagedCache(kc, vc)
+    cache.append(k, v, table, idx=idx, S=S, pos=out_pos, rope=rope)
+    assert cache.status() == dart.DART_OK and ctx.status() == dart.DART_OK
+    assert torch.equal(out_hidden, torch.gather(hidden, 1, idx.long()[..., None].expand(-1, -1, Hq * D)))
+    t = torch.arange(S_out, device="cuda")
+    for b in range(B):
+        page = table[b].long()[t // 16]
+        assert torch.equal(kc[page, :, t % 16].reshape(S_out, -1), kept_keys[b])  # the same rows, rotated on the way
+        assert torch.equal(vc[page, :, t % 16], v.view(B, S, Hk, D)[b, idx[b].long()])
+    ctx.close()
