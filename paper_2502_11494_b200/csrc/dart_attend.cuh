@@ -519,7 +519,8 @@ __global__ void __launch_bounds__(kNarrowWarps * 32, 1) attend_narrow_kernel(con
                     s[n][i] = exp2_approx(s[n][i] - top[i >> 1]);
                     l[i >> 1] += s[n][i];
                 }
-                // (weights enter the second product in the cache's type: half a step of it, relative, per token)
+                // (weights enter the second product in the cache's type: half a step of it, relative, per token; fp16 weights below 2^-14 by
+                // 2^-25 of the row's largest so far, those below that not at all, while the sum counts them: some 2^-25 of |v| each)
                 pa[n >> 1][(n & 1) * 2] = pack2<T>(s[n][0], s[n][1]);
                 pa[n >> 1][(n & 1) * 2 + 1] = pack2<T>(s[n][2], s[n][3]);
             }

@@ -572,7 +572,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                         const float a0 = exp2_approx(fmaf(s[c * 32 + 2 * i], p.scale_log2, -ref)), a1 = exp2_approx(fmaf(s[c * 32 + 2 * i + 1], p.scale_log2, -ref));
                         const float a2 = exp2_approx(fmaf(s[c * 32 + 2 * i + 2], p.scale_log2, -ref)), a3 = exp2_approx(fmaf(s[c * 32 + 2 * i + 3], p.scale_log2, -ref));
                         l0 += a0, l1 += a1, l2 += a2, l3 += a3;
-                        // (weights enter the second product in the cache's type: half a step of it, relative, per token)
+                        // (weights enter the second product in the cache's type: half a step of it, relative, per token; fp16 weights below
+                        // 2^-14 by 2^-25, where the row's largest is 1 to 2^8, while the sum counts them whole)
                         w16[i] = pack2<T>(a0, a1), w16[i + 1] = pack2<T>(a2, a3);
                     }
                     tmem_st16(s_at + c * 16, w16);

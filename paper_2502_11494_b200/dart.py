@@ -391,7 +391,7 @@ def _vector(t, name, size, dtype, device):
 class Rope:
     """A position rotation: the first ``2 * len(inv_freq)`` elements of a head turn by ``pos * inv_freq``, pairs being
     ``(i, i + half)`` or, ``interleaved``, ``(2i, 2i + 1)``.  ``sections``: pairs per position axis (vision tokens in time,
-    height and width)."""
+    height and width).  Positions [axes, N] have rows of their own: ``pos.expand(3, N)`` of text tokens is to be made contiguous."""
 
     def __init__(self, inv_freq, interleaved=False, sections=None):
         import torch
@@ -464,7 +464,8 @@ def norm_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6,
 
 class PagedCache:
     """A cache of keys and values in pages: two tensors [pages, heads, page_size, head_dim], the caller's.  A sequence's token
-    number s lies in page ``table[sequence, s // page_size]``."""
+    number s lies in page ``table[sequence, s // page_size]``.  ``append`` fills pages of any size and head_dim up to 256 (a multiple of
+    8); ``attend`` reads head_dim 64 and 128 and page_size 16 to 1024, a power of two, and refuses others."""
 
     def __init__(self, k, v):
         torch = _with_torch()
@@ -505,7 +506,7 @@ class PagedCache:
         """Rows of keys and values [N, heads, D] behind the ``start`` tokens that each sequence already has.  ``cu_rows``
         [sequences + 1]: ragged numbers of rows (None: equally many).  ``idx`` (a reduction's out_idx, flat or [B, S_out]): take row
         b * S + idx[n] for packed row n.  The keys are normalised (``k_weight``) and rotated (``rope``, at ``pos`` or at the slots)
-        on the way."""
+        on the way; a slot is the number in the sequence's own pages, so that tokens behind a shared prefix need ``pos``."""
         dev, dtype, D = self.device, self.dtype, self.head_dim
         tp, ts, n_seq, table = self._table(table, "table", stream)
         rows = k.shape[0]
