@@ -368,7 +368,7 @@ int dart_pivots_static(const void *keys, int B, int S, int d, int vis_offset, in
 /* A position rotation.  With half = rot_dim / 2 and angle_i = pos * inv_freq[i] (i < half), a head x becomes
  *   interleaved == 0:  x[i] cos_i - x[i + half] sin_i,  x[i + half] cos_i + x[i] sin_i
  *   interleaved != 0:  the same with elements 2i and 2i + 1;   elements from rot_dim on stay.
- * Angles are taken in fp64, so that far and negative positions lose nothing. */
+ * Angles are products in fp64, reduced to one turn there: off by 4e-7 of a radian at most at a position of 2^30, by less the nearer it is. */
 typedef struct {
     const float *inv_freq; /* [rot_dim / 2] device */
     int32_t rot_dim;       /* a multiple of 16, at most head_dim; 0: no rotation */

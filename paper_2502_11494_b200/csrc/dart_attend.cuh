@@ -6,8 +6,8 @@
 // Work.  The R = Hq / Hk query heads that share a KV head are rows of one product: row r = t R + (h mod R).  A segment is a
 // prefix (with the rows of all its group's sequences) or a sequence's own tokens (with its rows).  An ITEM is one KV head and one
 // tile of M rows of a segment; its KV tokens are cut into TILES.  All tiles of all items stand in one line, each item with kCost
-// tiles' worth of room before it (what beginning and ending a piece takes; wide tiles, room 1, 2, 3, 4: questions behind shared
-// images 391, 306, 282, 304 us, prefill 356, 335, 339, 349), and every worker takes an equal, contiguous share of it: no worker waits
+// tiles' worth of room before it (what beginning and ending a piece takes; wide tiles, room 1, 2, 3, 4, at 1965 MHz: questions behind
+// shared images 376, 296, 276, 296 us, prefill 327, 313, 324, 328), and every worker takes an equal, contiguous share of it: no worker waits
 // for another, and one long sequence fills the GPU as well as many short ones.  A prefix is read once per M rows of its whole group.  The lengths are only known on the device; every
 // CTA adds them up itself (a launch for it would cost more).
 // Joining.  An item that one worker held whole, with nothing else to join, is written at once.  A worker's first and last item may
@@ -331,7 +331,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -
 // what the joining launch merges anyway).  Keys and values of 32 tokens take turns in the ring; with three places of 8 KB and eight
 // warps 128 KB are on their way per SM, which covers the latency of HBM at its full rate.  Tokens behind the end of a sequence
 // are filled with zeros in shared memory, whatever their page holds: 0 * NaN would be NaN.
-// Measured: 64 sequences of 164 to 676 tokens, 32 heads of 128, 91 us = 5.5 TB/s; two of 99000 and 131072 tokens, 4 KV heads, 88 us = 5.8 TB/s (copy
+// Measured: 64 sequences of 164 to 676 tokens, 32 heads of 128, 88 us = 5.7 TB/s; two of 99000 and 131072 tokens, 4 KV heads, 85 us = 6.0 TB/s (copy
 // rate 6.55).  Room of 0, 2, 4 tiles an item: 1, 1, 3 % slower; L2 prefetch hints on the copies: no difference.
 constexpr int kNarrowM = 16, kNarrowTile = 32, kNarrowWarps = 8, kNarrowCost = 1, kNarrowLeast = 4;
 constexpr int kNarrowRing = 24576; // bytes of a warp's ring

@@ -45,7 +45,7 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 // ---- status words of calls without a context ------------------------------------------------------
 // An index, a page or a length outside its range.  Never over a wait that gave up (rows that are not valid say more): of the codes, 0 < CHECK <
 // TIMEOUT as unsigned numbers.  (One instruction that returns nothing: as atomicCAS or atomicMax, which the compiler first adds up over the
-// warp, it stood in the way of kernels that hardly ever come here: single tokens 13.0 -> 13.7 us, 92.5 -> 95.3.)
+// warp, it stood in the way of kernels that hardly ever come here: one sequence's single token 13.0 -> 13.7 us.)
 constexpr int kErrCheck = -8;
 __device__ __forceinline__ void report_check(int32_t *status)
 {

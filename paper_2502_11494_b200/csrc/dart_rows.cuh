@@ -5,9 +5,10 @@
 //   halves:       z[i] = y[i] cos_i - y[i + half] sin_i,      z[i + half]  = y[i + half] cos_i + y[i] sin_i
 //   interleaved:  the same with elements 2i and 2i + 1;  elements from 2 half on stay y.
 // Everything is held in fp32 and rounded once, when it is stored.  An angle is a product in fp64, reduced to one turn there
-// (rint of the number of turns), so that far positions lose nothing; what is left of it goes through sincospif in fp32.
+// (rint of the number of turns), so that far positions lose little (two products' roundings, 3 2^-53 of all turns); what is left of it goes
+// through sincospif in fp32.
 //
-// Bound by memory, with the SM's issue close behind (79 % of it): each value is read once and written once.  A thread owns both halves
+// Bound by memory, with the SM's issue close behind (77 % of it): each value is read once and written once.  A thread owns both halves
 // of eight rotated pairs (two 16-byte loads, two 16-byte stores) and needs nobody else's values but for the sum of squares (shuffles
 // among the 4 to 16 threads of a head).  A row's cosines and sines are taken once per block, into shared memory, and serve all of its
 // heads (per head they would be most of the kernel's instructions).  Both sides' weights kept in registers, 16 more: 5 % slower.

@@ -59,8 +59,8 @@ bool known_type(int dtype) { return dtype == DART_BF16 || dtype == DART_FP16; }
 bool head_rows_ok(int heads, int D, long long stride, int n_rows) { return heads >= 0 && (n_rows <= 1 || stride >= (long long)heads * D) && stride % 8 == 0 && stride >= 0; }
 
 // Few rows: one round of heads per block, a row's heads over several blocks.  Many rows: up to eight rows a block, so that a thread has
-// several rounds to overlap and the rows' angles serve all heads (43264 rows of 64 heads of 128: eight rounds 235 us, four 246, sixteen 235;
-// blocks of 256 threads 246, of 64 230, but 4 % slower on 18832 rows of 32 heads with sixteen rounds).
+// several rounds to overlap and the rows' angles serve all heads (43264 rows of 64 heads of 128 at 1965 MHz: eight rounds 230 us, four
+// 238, sixteen 230; blocks of 256 threads 242, of 64 229; 18832 rows of 32 heads: 60.1; 60.2, 61.2; 60.7, 60.0.  In long runs, under the power cap: 255 to 260).
 template <typename T, bool kPaged>
 int launch_rows(dart::rows::Params &p, cudaStream_t st)
 {
@@ -114,7 +114,7 @@ struct Layout {
 };
 
 // Rows of a tile by how many rows a segment has on average (the host knows the sizes, not the lengths).  64 sequences of 300 to 600 tokens,
-// 8 KV heads, in us: 8 rows each narrow 40, wide 53; 16 rows 36, 50; 32 rows 50, 52; 64 rows 77, 55; 128 rows wide 62, pairs 67; 192 rows 90, 79.
+// 8 KV heads, in us: 8 rows each narrow 40, wide 51; 16 rows 35, 47; 32 rows 47, 49; 64 rows 74, 52; 128 rows wide 58, pairs 64; 192 rows 81, 74.
 // A wide tile holds whole tokens, so that a copy can fetch its queries.
 Form form_of(long long rows, long long segments, long long R)
 {
@@ -143,8 +143,9 @@ Layout attend_layout(const dart_cache *c, const dart_attend_args *a, int sms)
     const long long R = a->n_q_heads / c->n_heads;
     Form own = form_of(a->n_rows * R, a->n_seq, R);
     const Form shared = a->n_groups > 0 ? form_of(a->n_rows * R, a->n_groups, R) : own;
-    // Few sequences go along with their prefixes: one launch instead of two (a prefix of 18432 tokens, 28 query heads, 4 KV heads: 16 sequences 40.6
-    // -> 31.6 us, 32 sequences 41.9 -> 36.9; 64 sequences, more than a worker each, 52.7 and, all in tiles of 256 rows, 55).
+    // Few sequences go along with their prefixes: one launch instead of two (a prefix of 18432 tokens, 28 query heads, 4 KV heads: 16 sequences 43.0
+    // -> 32.1 us, 32 sequences 44.2 -> 35.9; more sequences than workers are left to a
+    // launch of their own, though this prefix, in tiles of 256 rows, would take 48 along in 48.1 instead of 51.5 us, 64 in 52.7 instead of 56.0).
     if (own == NARROW && shared != NARROW && (long long)a->n_seq * c->n_heads <= (shared == WIDE ? 2 : 1) * sms) own = shared;
     L.n = own == shared ? 1 : 2;
     L.launch[0].prefix = a->n_groups > 0, L.launch[0].own = own == shared, L.launch[0].form = shared;

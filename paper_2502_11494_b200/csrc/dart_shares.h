@@ -18,7 +18,7 @@ struct Shares {
 
     // A line of `line` tiles in `items` items (0 <= line <= kLongestLine) for n workers.  least: the most that a share's least size may be.
     // Long items in small shares are slower to join than to read (narrow form, us a call, shares of 1, 2, 4 tiles at least: one sequence of
-    // 300 tokens 12.8, 14.1, 18.0; of 6000 23.2, 19.8, 20.6; of 24000 34.5, 34.5, 31.6): a tile for each 64 of an item, up to `least`.
+    // 300 tokens 16, 17, 18; of 6000 19.6, 18.0, 19.9; of 24000 34.5, 34.5, 27.5): a tile for each 64 of an item, up to `least`.
     static DART_BOTH Shares of(int line, long long items, int n, int least)
     {
         Shares s;
