@@ -472,7 +472,7 @@ typedef struct {
  * lengths; 0 for arguments that dart_attend refuses and for n_rows 0 (which does nothing).
  * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, else UNSUPPORTED; fewer than 2^30 (row, head) pairs and 2^31 cached (head, token)
  * pairs.  What the lengths ask for is known on the device only: 2^31 pairs of a tile of 16 or 128 rows of a KV head and a tile of 32 or 128 tokens (a prompt
- * of two million rows and 32 heads) are reported there.  Keys and values of visible tokens must be finite, and scores of finite queries below 2^27 in size (fp32 tells
+ * of two million rows and 32 heads) are reported there.  Keys and values of tokens that any row sees must be finite (a value that is not reaches the rows of its tile that do not see it), and scores of finite queries below 2^27 in size (fp32 tells
  * no weights apart long before); whatever else lies in the pages has no influence.
  * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED, NOMEM (workspace too small), CUDA.
  */

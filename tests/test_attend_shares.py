@@ -45,7 +45,7 @@ def shares(tmp_path_factory):
     cxx = shutil.which("g++") or shutil.which("c++")
     if cxx is None:
         pytest.skip("no C++ compiler")
-    subprocess.check_call([cxx, "-std=c++17", "-O1", "-fsanitize=signed-integer-overflow", "-fno-sanitize-recover", "-I",
+    subprocess.check_call([cxx, "-std=c++17", "-O1", "-fsanitize=signed-integer-overflow", "-fsanitize-undefined-trap-on-error", "-I",
                            os.path.join(ROOT, "paper_2502_11494_b200", "csrc"), "-o", str(d / "shares"), str(src)])
 
     def run(cases):
