@@ -458,9 +458,9 @@ typedef struct {
     float scale;                  /* > 0 */
     int32_t wait_limit;           /* 0: default (2 s); > 0: time limit in microseconds of every bounded device-side wait */
     int32_t *status;              /* [4] device, or NULL.  status[0] becomes DART_ERR_CHECK where a page of a visible token is outside the
-                                     cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), or offsets
-                                     that do not ascend name more rows than there are, or the work has 2^31 pairs of a tile of rows and a tile of tokens or
-                                     more (nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
+                                     cache (it then reads as zeros), a length is negative or longer than its table row (it is cut), cu_q or
+                                     cu_group does not ascend within the rows or sequences that there are, or the work has 2^31 pairs of a
+                                     tile of rows and a tile of tokens or more (then nothing is written); DART_ERR_TIMEOUT where a bounded wait gave up (rows are then not valid):
                                      status[1..3] say which wait, item and CTA.  A status that is not 0 stays, but for TIMEOUT over CHECK */
     int32_t test_withhold;        /* testing only: 1 withholds one hand-over inside the kernel that waits, 2 lets the wait for a tile's queries
                                      give up at once, while their copy may still be under way */

@@ -109,6 +109,13 @@ __device__ inline Seg load_seg(const Params &p, int s)
     return g;
 }
 
+// Whether a segment's offsets ascend inside what there is: others name rows twice (two workers would write them), or rows that are not there.
+__device__ __forceinline__ bool ascends(const Params &p, int s)
+{
+    const int32_t *cu = s < p.n_prefix ? p.cu_group + s : p.cu_q + (s - p.n_prefix);
+    return (s >= p.n_prefix && !p.cu_q) || (0 <= cu[0] && cu[0] <= cu[1] && cu[1] <= (s < p.n_prefix ? p.n_seq : p.n_rows));
+}
+
 // Own tokens that row t sees.
 __device__ __forceinline__ int sees(const Seg &g, int t) { return g.prefix ? g.len : clamp(g.len - g.n_q + t + 1, 0, g.len); }
 // ... and what the last row of a tile sees: how far its KV tiles go.  A sequence's rows have a tile even if they see nothing (it
@@ -162,6 +169,7 @@ __device__ void plan(const Params &p, PlanShared<kWorkers> &sh)
     for (int s = s0; s < s1; ++s) {
         g = load_seg<true>(p, s);
         items += p.Hk * (long long)g.nmb, room += room_of<kTile, kCost>(p, g);
+        if (!ascends(p, s)) room += 1ll << 32; // a line too long: reported, and nothing is done
     }
     long long i_sum = items, r_sum = room;
 #pragma unroll 1
@@ -698,6 +706,7 @@ __global__ void __launch_bounds__(kWarps > 1 ? kWarps * 32 : 128) attend_join_ro
         int s = b, row0;
         if (kind == 0) {
             if (p.n_groups == 0) continue;
+            if (j.from[0].item_base[j.n_seg[0]] < 0) return;
             if (b < p.cu_group[0] || b >= p.cu_group[p.n_groups]) continue; // in no group
             int lo = 0, hi = p.n_groups;
             while (hi - lo > 1) {

@@ -526,6 +526,27 @@ def test_tables_that_are_the_last_columns_of_wider_ones():
     assert c.cache.status() == dart.DART_ERR_CHECK and torch.equal(out, cut)
 
 
+@pytest.mark.parametrize("q", [1, 30])
+@pytest.mark.parametrize("which,offsets", [
+    ("q", [0, 2, 1, 4]), ("q", [0, 3, 3, 5]), ("q", [-1, 1, 2, 4]), ("q", [0, 0, 5, 4]), ("q", [4, 0, 4, 0]), ("q", [0, 2**31 - 1, 2, 4]),
+    ("group", [0, 2, 1, 3]), ("group", [0, 1, 2, 4]), ("group", [-1, 1, 2, 3]), ("group", [3, 0, 0, 3]), ("group", [1, 1, 1, 0]),
+])
+@pytest.mark.parametrize("prefixes", [False, True])
+def test_offsets_that_cannot_be_are_reported(which, offsets, prefixes, q):
+    """Offsets that descend, or leave the rows or sequences that there are: reported, and not a row is written, in no form and by no join."""
+    if which == "group" and not prefixes:
+        pytest.skip("no groups")
+    c = Case(8, 2, 64, 16, "bf16", [(q, 90), (2 * q, 200), (q, 50)], groups=[(1, 300), (1, 40), (1, 0)] if prefixes else [])
+    bad = torch.tensor([x * q if abs(x) < 2**30 else x for x in offsets] if which == "q" else offsets, dtype=torch.int32, device="cuda")
+    cu = bad if which == "q" else c.cu_q
+    prefix = (*c.prefix[:2], bad) if which == "group" else c.prefix
+    out, lse = torch.full_like(c.q, 7.0), torch.full((c.n, 8), 7.0, device="cuda")
+    c.cache.attend(c.q, c.table, c.kv_len, cu_q=cu, prefix=prefix, out=out, lse=lse)
+    assert c.cache.status() == dart.DART_ERR_CHECK
+    assert bool((out == 7).all()) and bool((lse == 7).all())
+    c.check()
+
+
 def test_threads_call_at_once():
     import threading
 
