@@ -471,9 +471,10 @@ typedef struct {
  * it; calls that may overlap (other streams, captured graphs) need one each.  The size depends on sizes only, not on
  * lengths; 0 for arguments that dart_attend refuses and for n_rows 0 (which does nothing).
  * Limits: head_dim 64 or 128, page_size a power of two from 16 to 1024, else UNSUPPORTED; fewer than 2^30 (row, head) pairs and 2^31 cached (head, token)
- * pairs.  What the lengths ask for is known on the device only: 2^31 pairs of a tile of 16 or 128 rows of a KV head and a tile of 32 or 128 tokens (a prompt
- * of two million rows and 32 heads) are reported there.  Keys and values of tokens that any row sees must be finite (a value that is not reaches the rows of its tile that do not see it), and scores of finite queries below 2^27 in size (fp32 tells
- * no weights apart long before); whatever else lies in the pages has no influence.
+ * pairs.  What the lengths ask for is known on the device only: 2^31 pairs of a tile of 16 or 128 rows of a KV head and a tile of 32 or 128 tokens (a
+ * prompt of two million rows and 32 heads) are reported there.
+ * Keys and values of tokens that any row sees must be finite (a value that is not reaches the rows of its tile that do not see it), and scores of
+ * finite queries below 2^27 in size (fp32 tells no weights apart long before); whatever else lies in the pages has no influence.
  * Allocates nothing and does not synchronise.  Errors: NULL, BAD_SHAPE, ALIGN, ALIAS, UNSUPPORTED, NOMEM (workspace too small), CUDA.
  */
 size_t dart_attend_workspace(const dart_cache *cache, const dart_attend_args *args);
